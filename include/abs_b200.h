@@ -281,6 +281,91 @@ int abs_lsq_gradient(const void* X, const float* y, const void* w, const int* id
 int abs_lsq_gradient_noalloc(const void* X, const float* y, const void* w, const int* idx, int n, int B,
                              int d, int dtype, float* g_out, float* loss_out, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Stand-alone operations on the layers of a network (the paper has no counterpart beyond the affine
+ * layers of Eq. 2): what a caller needs to evaluate a trained model on data, and to train networks
+ * of its own next to a run.  They share these rules:
+ *  - `dtype` is ABS_FP32 (float everywhere) or ABS_BF16_FP32MASTER (bf16 matrices, vectors and
+ *    gradients); sums, statistics and activations are formed in fp32 and a result is rounded once,
+ *    where it is stored, unless a function says otherwise.
+ *  - Matrices are row-major device memory with a row pitch (ld*, in elements, at least the number
+ *    of columns); what lies between the rows and behind the last one is neither read nor written.
+ *    Any alignment of the stored type is accepted.
+ *  - A result may not overlap an operand or another result, except where a function says so.
+ *  - All pointers belong to the current device, work is enqueued on `stream`, nothing is
+ *    allocated and nothing synchronises, so every call can be captured into a graph.  The first
+ *    call on a device should come before any stream capture.
+ *  - `scratch` is device memory of the size that the function's *_scratch_bytes twin reports,
+ *    256-byte aligned; its contents do not matter and are undefined afterwards.  Calls that may
+ *    overlap on the GPU (other streams, other threads, two captured graphs) need a scratch each.
+ *  - Sums have a fixed order: the same call on the same device type gives the same bits.
+ *  - Zero rows (samples) are allowed: nothing but zero parameter gradients is written.
+ */
+
+/* activations */
+#define ABS_ACT_NONE 0
+#define ABS_ACT_RELU 1   /* max(z, 0); slope 0 at z = 0; a NaN counts as not positive */
+#define ABS_ACT_GELU 2   /* z Phi(z), Phi the normal distribution function */
+#define ABS_ACT_SILU 3   /* z / (1 + exp(-z)) */
+
+/* Affine layer z = x W + b, y = act(z) + residual.
+ * x [rows][n_in], w [n_in][n_out] (the parameter layout of w0 and abs_get_params), bias [n_out] or
+ * NULL, residual [rows][n_out] or NULL, y [rows][n_out]; pre [rows][n_out] receives z (the backward
+ * pass needs it unless act is ABS_ACT_NONE) or is NULL.  y may be the same matrix as residual.
+ * rows in [0, 2^31), n_in and n_out in [1, 2^20]. */
+int abs_linear(const void* x, long long ldx, const void* w, long long ldw, const void* bias, const void* residual,
+               long long ldr, void* y, long long ldy, void* pre, long long ldp, long long rows, int n_in, int n_out,
+               int act, int dtype, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Gradients of the affine layer: with dz = dy * act'(pre) (pre may be NULL for ABS_ACT_NONE),
+ * dx = dz W^T, dw = x^T dz, db = column sums of dz; each of dx, dw, db may be NULL.  The residual's
+ * gradient is dy itself.  With ABS_BF16_FP32MASTER dz is rounded to bf16 where it enters the two
+ * matrix products (db sums it unrounded). */
+int abs_linear_grad(const void* dy, long long lddy, const void* x, long long ldx, const void* w, long long ldw,
+                    const void* pre, long long ldp, void* dx, long long lddx, void* dw, long long lddw, void* db,
+                    long long rows, int n_in, int n_out, int act, int dtype, void* scratch, size_t scratch_bytes,
+                    void* stream);
+
+/* Scratch of abs_linear (grad = 0) or abs_linear_grad (grad = 1).  aligned = 1 if every matrix of
+ * the call starts on a 16-byte boundary and has a row pitch that is a multiple of 16 bytes; 0
+ * covers every call. */
+int abs_linear_scratch_bytes(long long rows, int n_in, int n_out, int act, int dtype, int grad, int aligned, size_t* out);
+
+/* Dropout with a mask that is never stored: y = (kept ? x * s : 0) + residual (NULL: none), on
+ * matrices [rows][cols].  Element (row, col) is kept iff h >= T, where T = p * 65536 rounded to the
+ * nearest integer (p in [0, 1]) and h is 16-bit half (col mod 8) of the Philox4x32-10 block with counter
+ * (col / 8, row, 2, call) and key `seed` (halves in the order word 0 low, word 0 high, word 1 low,
+ * ...; word 2 of the counter is 0 and 1 in the draws of a run); s = 65536 / (65536 - T), so that the
+ * expectation is exact for the probability that is used.  A dropped element contributes 0 whatever
+ * its value.  The gradient is the same call on dy without residual.  y may be the same matrix as x
+ * or residual.  rows in [0, 2^32), cols in [1, 2^31). */
+int abs_dropout(const void* x, long long ldx, const void* residual, long long ldr, void* y, long long ldy,
+                long long rows, long long cols, double p, unsigned long long seed, unsigned int call, int dtype,
+                void* stream);
+
+/* Group normalisation of channels-last maps (the [H][W][C] order of ABS_CNN) with an activation:
+ * sample n, position i, channel c at x[n * xs + i * xp + c]; a group is channels / groups
+ * consecutive channels, mean and variance are those of the group over all positions of the sample,
+ * rstd = 1 / sqrt(variance + eps), u = (x - mean) rstd w[c] + b[c], y = act(u).  w and b: [channels]
+ * or NULL (1 and 0).  mean, rstd: float [samples][groups], or both NULL.  y has pitches ys, yp and may
+ * be the same maps as x.  samples and positions in [0, 2^31), channels in [1, 2^20] and a multiple of
+ * groups, eps > 0. */
+int abs_group_norm(const void* x, long long xs, long long xp, const void* w, const void* b, void* y, long long ys,
+                   long long yp, float* mean, float* rstd, long long samples, long long positions, int channels,
+                   int groups, float eps, int act, int dtype, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Its gradients, from the mean and rstd that the forward pass stored: g = dy * act'(u),
+ * db[c] = sum g, dw[c] = sum g xh (xh = (x - mean) rstd), dx = rstd (g w - mean of g w over the group -
+ * xh * mean of g w xh over the group).  dx may be NULL, or the same maps as dy; dw and db may be NULL. */
+int abs_group_norm_grad(const void* dy, long long dys, long long dyp, const void* x, long long xs, long long xp,
+                        const void* w, const void* b, const float* mean, const float* rstd, void* dx, long long dxs,
+                        long long dxp, void* dw, void* db, long long samples, long long positions, int channels,
+                        int groups, int act, int dtype, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Scratch of abs_group_norm (grad = 0) or abs_group_norm_grad (grad = 1). */
+int abs_group_norm_scratch_bytes(long long samples, long long positions, int channels, int groups, int dtype, int grad,
+                                 size_t* out);
+
 /* How the context runs (the paper has no counterpart): *partials = number of fp32 partial sums
  * the Eq. 3 step adds up per parameter (0: one per selected worker), *row_block = padding unit of
  * a version group's gradient rows, *rows_cap = row capacity of the activation buffers,

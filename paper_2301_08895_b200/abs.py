@@ -27,6 +27,7 @@ FLAG_NO_OVERLAP = 2
 FLAG_NO_PERSISTENT = 8
 FLAG_NO_BULK_PIPELINE = 32
 FLAG_NO_FUSED_BACKWARD = 64
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 KC_NAMES = ("ctl", "gather", "fwd", "dgrad", "wgrad", "output", "lsq", "update", "rounds", "conv")
 
 
@@ -91,6 +92,14 @@ def lib():
         l.abs_lsq_gradient_noalloc.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                                C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p,
                                                C.c_void_p, C.c_void_p]
+        p, q, i, z = C.c_void_p, C.c_longlong, C.c_int, C.c_size_t
+        l.abs_linear.argtypes = [p, q, p, q, p, p, q, p, q, p, q, q, i, i, i, i, p, z, p]
+        l.abs_linear_grad.argtypes = [p, q, p, q, p, q, p, q, p, q, p, q, p, q, i, i, i, i, p, z, p]
+        l.abs_linear_scratch_bytes.argtypes = [q, i, i, i, i, i, i, C.POINTER(z)]
+        l.abs_dropout.argtypes = [p, q, p, q, p, q, q, q, C.c_double, C.c_ulonglong, C.c_uint, i, p]
+        l.abs_group_norm.argtypes = [p, q, q, p, p, p, q, q, p, p, q, q, i, i, C.c_float, i, i, p, z, p]
+        l.abs_group_norm_grad.argtypes = [p, q, q, p, q, q, p, p, p, p, p, q, q, p, p, q, q, i, i, i, i, p, z, p]
+        l.abs_group_norm_scratch_bytes.argtypes = [q, q, i, i, i, i, C.POINTER(z)]
         l.abs_get_plan.argtypes = [C.c_void_p, C.POINTER(C.c_int), C.POINTER(C.c_int),
                                    C.POINTER(C.c_int), C.POINTER(C.c_int)]
         l.abs_profile_start.argtypes = [C.c_void_p, C.c_int]
@@ -334,6 +343,208 @@ def lsq_gradient_noalloc(X, y, w, idx, g_out, loss_out, stream=None):
     _check(lib().abs_lsq_gradient_noalloc(X.data_ptr(), y.data_ptr(), w.data_ptr(), idx.data_ptr(), n, B, X.shape[1],
                                           BF16_FP32MASTER if X.dtype == torch.bfloat16 else FP32, g_out.data_ptr(),
                                           loss_out.data_ptr(), _raw_stream(torch, stream, X)))
+
+
+# ---- layer operations on torch CUDA tensors
+
+def _torch():
+    global _torch_mod, _STORED
+    if _torch_mod is None:
+        import torch
+        _torch_mod = torch
+        _STORED = {torch.float32: FP32, torch.bfloat16: BF16_FP32MASTER}
+    return _torch_mod
+
+
+_torch_mod = None
+_STORED = {}
+
+
+class _Call:
+    """The tensors of one call: one type, one device, which is made current for the call; their addresses, and the stream."""
+
+    def __init__(self, first, stream):
+        torch = _torch()
+        self.dtype = first.dtype
+        self.code = _STORED.get(first.dtype, -1)
+        if self.code < 0:
+            raise ValueError("expected float32 or bfloat16 tensors, got %s" % first.dtype)
+        self.device = first.get_device()
+        if self.device < 0:
+            raise ValueError("expected a tensor on a CUDA device, got one on %s" % first.device)
+        if stream is None:
+            self.stream = _raw_stream(torch, None, first)
+        else:
+            if stream.device_index != self.device:
+                raise ValueError("the stream belongs to device %d, the tensors to device %d" % (stream.device_index, self.device))
+            self.stream = stream.cuda_stream
+        self.owner = stream
+
+    def tensor(self, name, t, shape, dtype=None):
+        """Address of a tensor of this call (0: None) whose last dimension is contiguous."""
+        if t is None:
+            return 0
+        if t.dtype is not (dtype or self.dtype) or t.get_device() != self.device:
+            raise ValueError("%s: expected %s on cuda:%d, got %s on %s" % (name, dtype or self.dtype, self.device, t.dtype, t.device))
+        if t.shape != shape:
+            raise ValueError("%s: expected shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+        if shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError("%s: the last dimension must be contiguous" % name)
+        return t.data_ptr()
+
+    def matrix(self, name, t, rows, cols):
+        """(address, row pitch) of a matrix."""
+        ptr = self.tensor(name, t, (rows, cols))
+        return ptr, (t.stride(0) if ptr and rows > 1 else cols)
+
+    def maps(self, name, t, shape):
+        """(address, sample pitch, position pitch) of channels-last maps [samples, ..., channels]."""
+        ptr = self.tensor(name, t, shape)
+        if not ptr:
+            return 0, 0, 0
+        pitch, span = shape[-1], 1
+        for d in range(len(shape) - 2, 0, -1):       # positions: one common pitch
+            if shape[d] > 1:
+                if span == 1:
+                    pitch = t.stride(d)
+                elif t.stride(d) != pitch * span:
+                    raise ValueError("%s: the positions of a sample must have one common pitch" % name)
+                span *= shape[d]
+        return ptr, t.stride(0), pitch
+
+    def scratch(self, given, need):
+        """(address, bytes, tensor) of scratch: the caller's, or one allocated for the call on its stream."""
+        if given is not None:
+            if given.get_device() != self.device or not given.is_contiguous():
+                raise ValueError("scratch: expected a contiguous tensor on cuda:%d" % self.device)
+            return given.data_ptr(), given.numel() * given.element_size(), given
+        if not need:
+            return 0, 0, None
+        torch = _torch()
+        if self.owner is None:
+            t = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", self.device))
+        else:
+            with torch.cuda.stream(self.owner):
+                t = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", self.device))
+        return t.data_ptr(), need, t
+
+    def run(self, fn, *args):
+        torch = _torch()
+        if torch.cuda.current_device() == self.device:
+            _check(fn(*args))
+        else:
+            with torch.cuda.device(self.device):
+                _check(fn(*args))
+
+
+def linear_scratch_bytes(rows, n_in, n_out, act=ACT_NONE, dtype=BF16_FP32MASTER, grad=False, aligned=False):
+    """abs_linear_scratch_bytes: scratch of `linear` or `linear_grad`; aligned: every matrix starts on a 16-byte
+    boundary and has a row pitch that is a multiple of 16 bytes."""
+    out = C.c_size_t(0)
+    _check(lib().abs_linear_scratch_bytes(rows, n_in, n_out, act, dtype, int(grad), int(aligned), C.byref(out)))
+    return out.value
+
+
+def linear(x, w, bias, residual, y, act=ACT_NONE, pre=None, scratch=None, stream=None):
+    """abs_linear: y = act(x w + bias) + residual.  x [rows, n_in], w [n_in, n_out], bias [n_out] or None, residual
+    [rows, n_out] or None, y [rows, n_out], all float32 or all bfloat16, rows at any pitch; pre [rows, n_out] (or None)
+    receives x w + bias for `linear_grad`.  scratch: a contiguous tensor of `linear_scratch_bytes`, or None to have
+    one allocated on the call's stream."""
+    rows, n_in = x.shape
+    n_out = w.shape[1]
+    c = _Call(x, stream)
+    xp, ldx = c.matrix("x", x, rows, n_in)
+    wp, ldw = c.matrix("w", w, n_in, n_out)
+    bp = c.tensor("bias", bias, (n_out,))
+    rp, ldr = c.matrix("residual", residual, rows, n_out)
+    yp, ldy = c.matrix("y", y, rows, n_out)
+    pp, ldp = c.matrix("pre", pre, rows, n_out)
+    aligned = ((xp | wp | rp | yp | pp) | ((ldx | ldw | ldr | ldy | ldp) * x.element_size())) & 15 == 0
+    sp, sz, keep = c.scratch(scratch, linear_scratch_bytes(rows, n_in, n_out, act, c.code, False, aligned))
+    c.run(lib().abs_linear, xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, pp, ldp, rows, n_in, n_out, act, c.code, sp, sz, c.stream)
+
+
+def linear_grad(dy, x, w, pre, dx, dw, db, act=ACT_NONE, scratch=None, stream=None):
+    """abs_linear_grad: from dy [rows, n_out] the gradients dx [rows, n_in], dw [n_in, n_out] and db [n_out] of `linear`
+    (None: not wanted); pre as `linear` left it (None with ACT_NONE).  The residual's gradient is dy itself."""
+    rows, n_in = x.shape
+    n_out = w.shape[1]
+    c = _Call(x, stream)
+    gp, ldg = c.matrix("dy", dy, rows, n_out)
+    xp, ldx = c.matrix("x", x, rows, n_in)
+    wp, ldw = c.matrix("w", w, n_in, n_out)
+    pp, ldp = c.matrix("pre", pre, rows, n_out)
+    dxp, lddx = c.matrix("dx", dx, rows, n_in)
+    dwp, lddw = c.matrix("dw", dw, n_in, n_out)
+    dbp = c.tensor("db", db, (n_out,))
+    aligned = ((gp | xp | wp | pp | dxp | dwp) | ((ldg | ldx | ldw | ldp | lddx | lddw) * x.element_size())) & 15 == 0
+    sp, sz, keep = c.scratch(scratch, linear_scratch_bytes(rows, n_in, n_out, act, c.code, True, aligned))
+    c.run(lib().abs_linear_grad, gp, ldg, xp, ldx, wp, ldw, pp, ldp, dxp, lddx, dwp, lddw, dbp, rows, n_in, n_out, act, c.code,
+          sp, sz, c.stream)
+
+
+def dropout(x, residual, y, p, seed, call, stream=None):
+    """abs_dropout on matrices [rows, cols]: y = (kept ? x / (1 - p) : 0) + residual (or None); the mask is a function of
+    element, `seed` and `call` (the number of the application: below 2^32).  The gradient is the same call on dy."""
+    rows, cols = x.shape
+    c = _Call(x, stream)
+    xp, ldx = c.matrix("x", x, rows, cols)
+    rp, ldr = c.matrix("residual", residual, rows, cols)
+    yp, ldy = c.matrix("y", y, rows, cols)
+    if not 0 <= call < 1 << 32 or not 0 <= seed < 1 << 64:
+        raise ValueError("call must be in [0, 2^32) and seed in [0, 2^64)")
+    c.run(lib().abs_dropout, xp, ldx, rp, ldr, yp, ldy, rows, cols, p, seed, call, c.code, c.stream)
+
+
+def group_norm_scratch_bytes(samples, positions, channels, groups, dtype=BF16_FP32MASTER, grad=False):
+    """abs_group_norm_scratch_bytes: scratch of `group_norm` or `group_norm_grad`."""
+    out = C.c_size_t(0)
+    _check(lib().abs_group_norm_scratch_bytes(samples, positions, channels, groups, dtype, int(grad), C.byref(out)))
+    return out.value
+
+
+def _positions(shape):
+    n = 1
+    for d in shape[1:-1]:
+        n *= d
+    return n
+
+
+def group_norm(x, groups, w, b, y, mean, rstd, eps=1e-5, act=ACT_NONE, scratch=None, stream=None):
+    """abs_group_norm: y = act(group_norm(x) w + b) on channels-last maps [samples, ..., channels]; w, b [channels] or
+    None; mean, rstd float32 [samples, groups] for `group_norm_grad`, or both None."""
+    c = _Call(x, stream)
+    shape = x.shape
+    n, pos, ch = shape[0], _positions(shape), shape[-1]
+    xp, xs, xq = c.maps("x", x, shape)
+    yp, ys, yq = c.maps("y", y, shape)
+    wp, bp = c.tensor("w", w, (ch,)), c.tensor("b", b, (ch,))
+    f32 = _torch().float32
+    mp, rp = c.tensor("mean", mean, (n, groups), f32), c.tensor("rstd", rstd, (n, groups), f32)
+    if n > 1 and ((mp and mean.stride(0) != groups) or (rp and rstd.stride(0) != groups)):
+        raise ValueError("mean and rstd must be contiguous")
+    sp, sz, keep = c.scratch(scratch, group_norm_scratch_bytes(n, pos, ch, groups, c.code, False))
+    c.run(lib().abs_group_norm, xp, xs, xq, wp, bp, yp, ys, yq, mp, rp, n, pos, ch, groups, eps, act, c.code, sp, sz, c.stream)
+
+
+def group_norm_grad(dy, x, groups, w, b, mean, rstd, dx, dw, db, act=ACT_NONE, scratch=None, stream=None):
+    """abs_group_norm_grad: dx (or None), dw and db [channels] (or None) of `group_norm` from dy and the mean and rstd
+    that the forward pass stored."""
+    c = _Call(x, stream)
+    shape = x.shape
+    n, pos, ch = shape[0], _positions(shape), shape[-1]
+    gp, gs, gq = c.maps("dy", dy, shape)
+    xp, xs, xq = c.maps("x", x, shape)
+    dxp, dxs, dxq = c.maps("dx", dx, shape)
+    wp, bp = c.tensor("w", w, (ch,)), c.tensor("b", b, (ch,))
+    dwp, dbp = c.tensor("dw", dw, (ch,)), c.tensor("db", db, (ch,))
+    f32 = _torch().float32
+    mp, rp = c.tensor("mean", mean, (n, groups), f32), c.tensor("rstd", rstd, (n, groups), f32)
+    if n > 1 and ((mp and mean.stride(0) != groups) or (rp and rstd.stride(0) != groups)):
+        raise ValueError("mean and rstd must be contiguous")
+    sp, sz, keep = c.scratch(scratch, group_norm_scratch_bytes(n, pos, ch, groups, c.code, True))
+    c.run(lib().abs_group_norm_grad, gp, gs, gq, xp, xs, xq, wp, bp, mp, rp, dxp, dxs, dxq, dwp, dbp, n, pos, ch, groups, act,
+          c.code, sp, sz, c.stream)
 
 
 def trace_rows(tr):

@@ -9,10 +9,10 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libabs_b200.so")
 STAMP = os.path.join(HERE, "libabs_b200.so.stamp")
-SOURCES = ["abs_api.cu", "ops.cu"]
+SOURCES = ["abs_api.cu", "ops.cu", "linear.cu", "dropout.cu", "groupnorm.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--expt-relaxed-constexpr", "--expt-extended-lambda",
-              "-Xcompiler", "-fPIC", "-shared", "-cudart", "shared"]
+              "-Xcompiler", "-fPIC", "-shared", "-cudart", "shared", "--threads", "0"]
 
 
 def _digest():

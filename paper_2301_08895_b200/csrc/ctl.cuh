@@ -3,24 +3,9 @@
 // integer decided by exact arithmetic, so the trace is reproducible bit for bit.
 #pragma once
 #include "common.cuh"
+#include "philox.cuh"
 
 namespace absb {
-
-// ---------------------------------------------------------------------------------------------
-// Philox4x32-10 (Salmon et al., SC'11): ten rounds of two 32x32->64 multiplies, with the key
-// advanced by Weyl constants between rounds.
-__device__ __forceinline__ void philox4x32_10(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3,
-                                              uint32_t k0, uint32_t k1, uint32_t out[4]) {
-#pragma unroll
-  for (int r = 0; r < 10; ++r) {
-    const uint32_t hi_a = __umulhi(0xD2511F53u, c0), lo_a = 0xD2511F53u * c0;
-    const uint32_t hi_b = __umulhi(0xCD9E8D57u, c2), lo_b = 0xCD9E8D57u * c2;
-    const uint32_t n0 = hi_b ^ c1 ^ k0, n2 = hi_a ^ c3 ^ k1;
-    c0 = n0; c1 = lo_b; c2 = n2; c3 = lo_a;
-    k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
-  }
-  out[0] = c0; out[1] = c1; out[2] = c2; out[3] = c3;
-}
 
 // Series logarithm that defines the exponential job times: u = m 2^e with m in [sqrt(1/2),
 // sqrt(2)), s = (m-1)/(m+1), ln u = e ln2 + 2s(1 + s^2/3 + ... + s^22/23).  Each step is one

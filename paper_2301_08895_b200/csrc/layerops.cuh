@@ -1,0 +1,143 @@
+// What the stand-alone layer operations share: argument checks, launches, activations, vector loads.
+#pragma once
+#include <math.h>
+
+#include "common.cuh"
+
+namespace absb {
+
+void set_last_error(const char* text);   // abs_api.cu: text returned by abs_last_error()
+
+namespace layer {
+
+constexpr int MAX_DEVICES = 64;
+
+int fail(int code, const char* fmt, ...);            // linear.cu
+// Properties of the current device, looked up once per device: ABS_OK, or an error with its text.
+int current_device(int* device, int* sms);           // linear.cu
+
+// A kernel that uses more than 48 KB of dynamic shared memory says so once per device.
+template <typename... KArgs>
+cudaError_t allow_smem(void (*kernel)(KArgs...), size_t bytes) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+// Launch that may start while the kernel in front of it drains: every kernel of these operations waits for that one
+// before it reads or writes anything.
+template <typename... KArgs, typename... Args>
+cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+// ---- device memory of a matrix: rows of `cols` elements, `ld` apart
+struct Span {
+  uintptr_t lo, hi;        // first byte and the byte behind the last one
+  long long ld, row;       // pitch and row length in bytes
+};
+inline Span span(const void* p, long long rows, long long cols, long long ld, size_t esz) {
+  Span s = {(uintptr_t)p, (uintptr_t)p, (long long)(ld * (long long)esz), (long long)(cols * (long long)esz)};
+  if (p && rows > 0) s.hi += (uintptr_t)((rows - 1) * s.ld + s.row);
+  return s;
+}
+// Whether two matrices share a byte; column ranges of one buffer (equal pitches) do not.
+inline bool overlap(const Span& a, const Span& b) {
+  if (a.lo == a.hi || b.lo == b.hi || a.hi <= b.lo || b.hi <= a.lo) return false;
+  if (a.ld != b.ld || a.ld <= 0) return true;
+  const long long d = (long long)((b.lo >= a.lo ? b.lo - a.lo : a.ld - (a.lo - b.lo) % a.ld) % a.ld);   // b's column offset from a
+  return d < a.row || d + b.row > a.ld;
+}
+
+// ---- activations
+__device__ __forceinline__ float normal_cdf(float z) { return 0.5f * erfcf(-0.70710678118654752f * z); }
+
+template <int ACT> __device__ __forceinline__ float act_value(float z) {
+  if (ACT == ABS_ACT_RELU) return fmaxf(z, 0.f);
+  if (ACT == ABS_ACT_GELU) return z * normal_cdf(z);
+  if (ACT == ABS_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
+  return z;
+}
+template <int ACT> __device__ __forceinline__ float act_slope(float z) {
+  if (ACT == ABS_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+  if (ACT == ABS_ACT_GELU) return normal_cdf(z) + z * (0.39894228040143268f * __expf(-0.5f * z * z));
+  if (ACT == ABS_ACT_SILU) {
+    const float s = __fdividef(1.f, 1.f + __expf(-z));
+    return s * (1.f + z * (1.f - s));
+  }
+  return 1.f;
+}
+
+// ---- VE consecutive stored values in one access (16 bytes, or one element), and as binary32
+template <typename T, int VE> struct Pack;
+template <> struct Pack<float, 4> {
+  float4 q;
+  __device__ __forceinline__ void load(const float* p) { q = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<float4*>(p) = q; }
+  __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w; }
+  __device__ __forceinline__ void set(const float (&v)[4]) { q = make_float4(v[0], v[1], v[2], v[3]); }
+};
+template <> struct Pack<__nv_bfloat16, 8> {
+  uint4 q;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { q = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = q; }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { v[2 * j] = __uint_as_float(u[j] << 16); v[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u); }
+  }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+    uint32_t u[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+      u[j] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    q = make_uint4(u[0], u[1], u[2], u[3]);
+  }
+};
+template <typename T> struct Pack<T, 1> {
+  T q;
+  __device__ __forceinline__ void load(const T* p) { q = *p; }
+  __device__ __forceinline__ void store(T* p) const { *p = q; }
+  __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = (float)q; }
+  __device__ __forceinline__ void set(const float (&v)[1]) { q = (T)v[0]; }
+};
+
+template <typename T> __device__ __forceinline__ T round_to(float v);
+template <> __device__ __forceinline__ float round_to<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 round_to<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// Division of x < 2^32 by a fixed d >= 1 (Granlund and Montgomery): q = (t + ((x - t) >> 1)) >> (l - 1) with
+// t = floor(m x / 2^32), l = ceil(log2 d), m = floor(2^32 (2^l - d) / d) + 1.
+struct Divisor {
+  uint32_t d, m;
+  int sh;
+  Divisor() = default;
+  __host__ explicit Divisor(uint32_t div) : d(div) {
+    int l = 0;
+    while (l < 32 && (1ull << l) < div) ++l;
+    m = (uint32_t)(((1ull << 32) * ((1ull << l) - div)) / div + 1);
+    sh = l;
+  }
+  __device__ __forceinline__ uint32_t div(uint32_t x) const {
+    if (sh == 0) return x;
+    const uint32_t t = __umulhi(m, x);
+    return (t + ((x - t) >> 1)) >> (sh - 1);
+  }
+};
+
+}  // namespace layer
+}  // namespace absb

@@ -1,0 +1,790 @@
+"""The layer operations (affine layer with its epilogue, dropout, group norm) against their definitions in 64 bits.
+
+Tolerances are bounds worked out from the operations' arithmetic, element by element: u = half a step of the storage type
+relative to the value (bf16 2^-8, fp32 2^-24), sums of K
+terms in fp32 that may truncate (2^-23 of the sum of magnitudes per addition), activations whose exponential is good to
+2^-20 at the arguments used, slopes |act'| <= 1.13 and |act''| <= 0.8.
+"""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import philox
+from paper_2301_08895_b200 import abs as gpu
+
+pytestmark = pytest.mark.gpu
+
+ACTS = [gpu.ACT_NONE, gpu.ACT_RELU, gpu.ACT_GELU, gpu.ACT_SILU]
+E20, E23 = 2.0 ** -20, 2.0 ** -23
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def dt(bf16):
+    torch = _torch()
+    return torch.bfloat16 if bf16 else torch.float32
+
+
+def half_step(bf16):
+    return _torch().finfo(dt(bf16)).eps / 2
+
+
+def act64(z, act):
+    torch = _torch()
+    if act == gpu.ACT_RELU:
+        return z.clamp(min=0)
+    if act == gpu.ACT_GELU:
+        return z * 0.5 * torch.special.erfc(-z / math.sqrt(2))
+    if act == gpu.ACT_SILU:
+        return z * torch.special.expit(z)
+    return z
+
+
+def slope64(z, act):
+    torch = _torch()
+    if act == gpu.ACT_RELU:
+        return (z > 0).double()
+    if act == gpu.ACT_GELU:
+        return 0.5 * torch.special.erfc(-z / math.sqrt(2)) + z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    if act == gpu.ACT_SILU:
+        s = torch.special.expit(z)
+        return s * (1 + z * (1 - s))
+    return torch.ones_like(z)
+
+
+def smooth(act):
+    return act in (gpu.ACT_GELU, gpu.ACT_SILU)
+
+
+class Held:
+    """A matrix (or maps) inside a larger buffer: row pitch, offset from an aligned start; what surrounds it is NaN and has to stay."""
+
+    def __init__(self, rows, cols, dtype, pad=0, offset=0, values=None):
+        torch = _torch()
+        self.buf = torch.full((offset + max(rows, 1) * (cols + pad) + 16,), float("nan"), dtype=dtype, device="cuda")
+        self.t = self.buf[offset:offset + max(rows, 1) * (cols + pad)].view(max(rows, 1), cols + pad)[:rows, :cols]
+        if values is not None:
+            self.t.copy_(values)
+        self.rows, self.cols, self.pad, self.offset = rows, cols, pad, offset
+
+    def surroundings_untouched(self):
+        torch = _torch()
+        mask = torch.ones_like(self.buf, dtype=torch.bool)
+        mask[self.offset:self.offset + max(self.rows, 1) * (self.cols + self.pad)].view(max(self.rows, 1), -1)[:self.rows, :self.cols] = False
+        return bool(torch.isnan(self.buf[mask]).all())
+
+
+def randn(g, *shape, scale=1.0, dtype=None):
+    torch = _torch()
+    return (torch.randn(*shape, generator=g, device="cuda") * scale).to(dtype or torch.float32)
+
+
+def gen(seed):
+    return _torch().Generator(device="cuda").manual_seed(seed)
+
+
+def within(got, want, tol):
+    torch = _torch()
+    got, bad = got.double(), None
+    err = (got - want).abs()
+    ok = bool((err <= tol).all())
+    if not ok:
+        i = int((err - tol).argmax())
+        bad = (i, float(got.flatten()[i]), float(want.flatten()[i]), float(tol.flatten()[i] if torch.is_tensor(tol) else tol))
+    assert ok, "at %d: got %.9g, want %.9g, tolerance %.3g" % bad
+
+
+# ------------------------------------------------------------------------------------------------ affine layer
+
+def linear_case(M, K, N, bf16, act, residual, pre, bias=True, pad=0, offset=0, seed=0, in_place=False):
+    torch = _torch()
+    g = gen(seed)
+    d, u = dt(bf16), half_step(bf16)
+    x = Held(M, K, d, pad, offset, randn(g, M, K, dtype=d))
+    w = Held(K, N, d, pad, offset, randn(g, K, N, scale=math.sqrt(2.0 / K), dtype=d))
+    b = randn(g, N, scale=0.3, dtype=d) if bias else None
+    r = Held(M, N, d, pad, offset, randn(g, M, N, dtype=d)) if residual else None
+    r64 = r.t.double().clone() if residual else 0.0
+    y = r if in_place else Held(M, N, d, pad, offset)
+    z = Held(M, N, d, pad, offset) if pre else None
+    gpu.linear(x.t, w.t, b, r.t if residual else None, y.t, act, pre=z.t if pre else None)
+    torch.cuda.synchronize()
+    x64, w64 = x.t.double(), w.t.double()
+    b64 = b.double() if bias else torch.zeros(N, dtype=torch.float64, device="cuda")
+    z64 = x64 @ w64 + b64
+    tz = (K + 4) * E23 * (x64.abs() @ w64.abs() + b64.abs())
+    a64 = act64(z64, act)
+    y64 = a64 + r64
+    ty = u * y64.abs() + 1.2 * tz + (E20 * (1 + z64.abs()) if smooth(act) else 0.0) + E23 * (a64.abs() + (r64.abs() if residual else 0.0))
+    within(y.t, y64, ty)
+    assert y.surroundings_untouched()
+    if pre:
+        within(z.t, z64, u * z64.abs() + 1.2 * tz)
+        assert z.surroundings_untouched()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("M,K,N", [
+    (1, 1, 1), (1, 784, 256), (1, 785, 10), (2, 7, 3), (5, 64, 1000), (8, 256, 64), (9, 256, 64), (16, 1000, 40), (17, 33, 129),
+    (127, 64, 64), (128, 128, 256), (129, 65, 257), (200, 8, 8), (300, 300, 123), (384, 512, 512), (513, 96, 10), (1000, 784, 256),
+    (33, 4096, 96), (40, 4099, 72)])
+def test_linear_sizes(M, K, N, bf16):
+    linear_case(M, K, N, bf16, gpu.ACT_RELU, False, False, seed=M + K + N)
+    linear_case(M, K, N, bf16, gpu.ACT_SILU, True, True, seed=M + K + N + 1)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("residual,pre,bias", [(False, False, False), (True, False, True), (False, True, False), (True, True, True)])
+def test_linear_epilogues(act, residual, pre, bias, bf16):
+    for M in (3, 150):
+        linear_case(M, 96, 136, bf16, act, residual, pre, bias, seed=act)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("pad,offset", [(8, 0), (8, 8), (1, 0), (0, 1), (3, 5), (2, 2), (4, 4)])
+def test_linear_pitches_and_alignment(pad, offset, bf16):
+    for M, K, N in ((1, 128, 64), (6, 120, 72), (150, 128, 256), (140, 72, 40)):
+        linear_case(M, K, N, bf16, gpu.ACT_GELU, True, True, pad=pad, offset=offset, seed=pad + 10 * offset)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_linear_adds_to_the_residual_in_place(bf16):
+    for M, N in ((1, 64), (130, 128), (130, 65)):
+        linear_case(M, 64, N, bf16, gpu.ACT_SILU, True, True, seed=5, in_place=True)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_linear_infinities_stay_in_their_rows_and_columns(bf16):
+    """An infinite activation reaches its row only, an infinite weight its column only, a NaN bias its column only."""
+    torch = _torch()
+    d = dt(bf16)
+    for M in (4, 140):
+        x = torch.ones(M, 72, device="cuda", dtype=d)
+        w = torch.ones(72, 130, device="cuda", dtype=d)
+        b = torch.zeros(130, device="cuda", dtype=d)
+        x[2, 71], w[0, 129], b[5] = float("inf"), float("inf"), float("nan")
+        y = torch.zeros(M, 130, device="cuda", dtype=d)
+        gpu.linear(x, w, b, None, y)
+        want = torch.full((M, 130), 72.0, device="cuda")
+        want[2, :], want[:, 129] = float("inf"), float("inf")
+        want[:, 5] = float("nan")
+        assert torch.equal(torch.nan_to_num(y.float(), nan=-1.0), torch.nan_to_num(want, nan=-1.0))
+
+
+def grad_case(M, K, N, bf16, act, pad=0, offset=0, seed=0, want=(True, True, True), differences=False):
+    torch = _torch()
+    g = gen(seed)
+    d, u = dt(bf16), half_step(bf16)
+    x = Held(M, K, d, pad, offset, randn(g, M, K, dtype=d))
+    w = Held(K, N, d, pad, offset, randn(g, K, N, scale=math.sqrt(2.0 / K), dtype=d))
+    dy = Held(M, N, d, pad, offset, randn(g, M, N, dtype=d))
+    b = randn(g, N, scale=0.3, dtype=d)
+    z = None
+    if act != gpu.ACT_NONE:
+        z = Held(M, N, d, pad, offset, (x.t.double() @ w.t.double() + b.double()).to(d))
+    dx = Held(M, K, d, pad, offset) if want[0] else None
+    dw = Held(K, N, d, pad, offset) if want[1] else None
+    db = torch.full((N,), float("nan"), device="cuda", dtype=d) if want[2] else None
+    gpu.linear_grad(dy.t, x.t, w.t, z.t if z else None, dx.t if dx else None, dw.t if dw else None, db, act)
+    torch.cuda.synchronize()
+    x64, w64, dy64 = x.t.double(), w.t.double(), dy.t.double()
+    dz = dy64 * slope64(z.t.double(), act) if z else dy64
+    tdz = (E20 * (1 + z.t.double().abs()) * dy64.abs() if smooth(act) else 0.0 * dz) + E23 * dz.abs()
+    tb = tdz + (M + 4) * E23 * dz.abs()
+    if bf16 and z:
+        tdz = tdz + u * dz.abs()                        # dz enters the products rounded to storage
+    if dx:
+        want_dx = dz @ w64.T
+        within(dx.t, want_dx, u * want_dx.abs() + 1.01 * ((tdz + (N + 4) * E23 * dz.abs()) @ w64.abs().T))
+        assert dx.surroundings_untouched()
+    if dw:
+        want_dw = x64.T @ dz
+        within(dw.t, want_dw, u * want_dw.abs() + 1.01 * (x64.abs().T @ (tdz + (M + 4) * E23 * dz.abs())))
+        assert dw.surroundings_untouched()
+    if db is not None:
+        want_db = dz.sum(0)
+        within(db, want_db, u * want_db.abs() + 1.01 * tb.sum(0))
+    if differences:
+        # directional derivative of L = sum dy act(x w + b) by central differences of the definition in 64 bits
+        # (step 1e-6: truncation 1e-12, rounding 1e-10 of L's terms); the gradients' own errors as above, summed.  Where the
+        # saved pre-activation is rounded (bf16) the gradient is the one at the rounded value: fp32 only.
+        assert not bf16
+        b64, h = b.double(), 1e-6
+        loss = lambda xx, ww, bb: float((dy64 * act64(xx @ ww + bb, act)).sum())           # noqa: E731
+        for got, at, tol in ((dx.t, 0, (tdz + (N + 4) * E23 * dz.abs()) @ w64.abs().T), (dw.t, 1, x64.abs().T @ (tdz + (M + 4) * E23 * dz.abs())),
+                             (db, 2, tb.sum(0))):
+            v = randn(g, *got.shape).double()
+            args = [x64, w64, b64]
+            lo, hi = list(args), list(args)
+            lo[at], hi[at] = args[at] - h * v, args[at] + h * v
+            num = (loss(*hi) - loss(*lo)) / (2 * h)
+            # pre is stored in fp32: the slope is taken up to 2^-24 |z| away, |act''| <= 0.8
+            shift = 0.8 * 2.0 ** -24 * (dy64 * z.t.double()).abs()
+            extra = {0: lambda: shift @ w64.abs().T, 1: lambda: x64.abs().T @ shift, 2: lambda: shift.sum(0)}[at]()
+            slack = float(((2 * tol + u * got.double().abs() + extra) * v.abs()).sum()) + 1e-8 * float((dy64 * z.t.double()).abs().sum())
+            assert abs(float((got.double() * v).sum()) - num) <= slack
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("M,K,N", [
+    (1, 1, 1), (1, 784, 256), (2, 7, 3), (7, 64, 10), (8, 256, 64), (31, 300, 123), (64, 64, 64), (129, 65, 257), (256, 128, 256),
+    (300, 400, 120), (513, 96, 10), (1000, 784, 256), (2000, 40, 24), (4100, 264, 8)])
+def test_linear_grad_sizes(M, K, N, bf16):
+    grad_case(M, K, N, bf16, gpu.ACT_NONE, seed=M)
+    grad_case(M, K, N, bf16, gpu.ACT_SILU, seed=M + 1)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("want", [(True, False, False), (False, True, False), (False, False, True), (True, True, False)])
+def test_linear_grad_of_chosen_operands(act, want, bf16):
+    grad_case(150, 72, 136, bf16, act, want=want, seed=act)
+    grad_case(150, 72, 136, bf16, act, want=want, pad=1, offset=3, seed=act)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("pad,offset", [(8, 0), (8, 8), (1, 0), (0, 1), (2, 2), (4, 4)])
+def test_linear_grad_pitches_and_alignment(pad, offset, bf16):
+    grad_case(140, 128, 72, bf16, gpu.ACT_GELU, pad=pad, offset=offset, seed=3)
+    grad_case(6, 72, 128, bf16, gpu.ACT_NONE, pad=pad, offset=offset, seed=4)
+
+
+@pytest.mark.parametrize("act", [gpu.ACT_GELU, gpu.ACT_SILU])
+def test_linear_grad_against_differences(act):
+    grad_case(37, 29, 23, False, act, seed=11, differences=True)
+
+
+def test_linear_without_rows():
+    torch = _torch()
+    for bf16 in (False, True):
+        d = dt(bf16)
+        w = torch.ones(16, 8, device="cuda", dtype=d)
+        gpu.linear(torch.empty(0, 16, device="cuda", dtype=d), w, None, None, torch.empty(0, 8, device="cuda", dtype=d))
+        dw, db = Held(16, 8, d, 3, 1), torch.ones(8, device="cuda", dtype=d)
+        gpu.linear_grad(torch.empty(0, 8, device="cuda", dtype=d), torch.empty(0, 16, device="cuda", dtype=d), w, None,
+                        torch.empty(0, 16, device="cuda", dtype=d), dw.t, db)
+        assert float(dw.t.abs().sum()) == 0.0 and float(db.abs().sum()) == 0.0 and dw.surroundings_untouched()
+
+
+def test_linear_of_matrices_behind_32_bit_offsets():
+    """Rows 2^30 elements apart: offsets of 2^31 elements and 2^32 bytes."""
+    torch = _torch()
+    pitch = 1 << 30
+    for K, N in ((64, 64), (63, 10)):
+        big = torch.empty(2 * pitch + 256, dtype=torch.bfloat16, device="cuda")
+        x = big.as_strided((3, K), (pitch, 1))
+        y = big.as_strided((3, N), (pitch, 1), 128)
+        x.copy_(randn(gen(1), 3, K, dtype=torch.bfloat16))
+        w = randn(gen(2), K, N, scale=0.1, dtype=torch.bfloat16)
+        gpu.linear(x, w, None, None, y)
+        want = x.double() @ w.double()
+        within(y, want, 2.0 ** -8 * want.abs() + (K + 4) * E23 * (x.double().abs() @ w.double().abs()))
+        del big, x, y
+        torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------------------------------------ dropout
+
+def keep_mask(rows, cols, p, seed, call):
+    """The mask by the oracle's generator."""
+    nblk = (cols + 7) // 8
+    blk, row = np.meshgrid(np.arange(nblk), np.arange(rows))
+    w = philox.philox4x32_10_blocks(blk.ravel(), row.ravel(), np.full(blk.size, 2), np.full(blk.size, call), philox.seed_key(seed))
+    half = np.stack([w & 0xFFFF, w >> 16], axis=-1).reshape(rows, nblk * 8)[:, :cols]
+    return half >= int(math.floor(p * 65536 + 0.5))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("rows,cols,p,pad,offset", [
+    (1, 1, 0.5, 0, 0), (1, 7, 0.3, 0, 0), (3, 8, 0.5, 0, 0), (5, 9, 0.5, 7, 0), (128, 256, 0.1, 0, 0), (33, 1000, 0.9, 0, 0), (200, 10, 0.5, 0, 1),
+    (64, 257, 0.25, 3, 5), (1, 100003, 0.5, 0, 0), (1000, 1, 0.5, 0, 0), (7, 512, 0.999999, 0, 0), (4, 64, 0.0, 8, 8), (4, 64, 1.0, 8, 0),
+    (300, 2056, 1.0 / 65536, 0, 0)])
+def test_dropout(rows, cols, p, pad, offset, residual, bf16):
+    torch = _torch()
+    d, u = dt(bf16), half_step(bf16)
+    g = gen(rows + cols)
+    x = Held(rows, cols, d, pad, offset, randn(g, rows, cols, dtype=d) + 3.0)
+    r = Held(rows, cols, d, pad, offset, randn(g, rows, cols, dtype=d)) if residual else None
+    y = Held(rows, cols, d, pad, offset)
+    seed, call = (0x123456789ABCDEF0 + rows) % 2 ** 64, 4000000000 + cols
+    gpu.dropout(x.t, r.t if r else None, y.t, p, seed, call % 2 ** 32)
+    keep = torch.from_numpy(keep_mask(rows, cols, p, seed, call % 2 ** 32)).cuda()
+    T = int(math.floor(p * 65536 + 0.5))
+    kept = torch.where(keep, x.t.double() * (65536.0 / (65536 - T) if T < 65536 else 0.0), torch.zeros((), dtype=torch.float64, device="cuda"))
+    want = kept + (r.t.double() if r else 0.0)
+    within(y.t, want, u * want.abs() + 2.0 ** -23 * kept.abs() + 2.0 ** -24 * want.abs())   # scale, product, sum; storage
+    if not r:
+        assert torch.equal(y.t != 0, keep & (x.t != 0))
+    assert y.surroundings_untouched()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_dropout_in_place_and_dropped_infinities(bf16):
+    torch = _torch()
+    d = dt(bf16)
+    for cols in (64, 61):
+        x = torch.ones(40, cols, device="cuda", dtype=d)
+        keep = torch.from_numpy(keep_mask(40, cols, 0.5, 7, 1)).cuda()
+        x[~keep] = float("nan")
+        x[0][~keep[0]] = float("inf")
+        gpu.dropout(x, None, x, 0.5, 7, 1)
+        assert torch.equal(x, torch.where(keep, 2.0, 0.0).to(d))
+        r = torch.full((40, cols), 3.0, device="cuda", dtype=d)
+        gpu.dropout(x, r, r, 0.5, 7, 1)
+        assert torch.equal(r, torch.where(keep, 7.0, 3.0).to(d))
+
+
+def test_dropout_gradient_is_the_same_call():
+    """L = sum c dropout(x): the derivative along v is sum dropout(c) v, exactly linear in x."""
+    torch = _torch()
+    g = gen(3)
+    x, c, v = (randn(g, 50, 77).double() for _ in range(3))
+    keep = torch.from_numpy(keep_mask(50, 77, 0.3, 9, 2)).cuda()
+    s = 65536.0 / (65536 - 19661)
+    dx = torch.empty(50, 77, device="cuda")
+    gpu.dropout(c.float(), None, dx, 0.3, 9, 2)
+    h = 1e-3
+    loss = lambda t: float((c.float().double() * torch.where(keep, t * s, 0.0)).sum())     # noqa: E731
+    num = (loss(x + h * v) - loss(x - h * v)) / (2 * h)
+    assert abs(float((dx.double() * v).sum()) - num) <= 1e-6 * float((dx.double() * v).abs().sum())
+
+
+def test_dropout_rate_and_calls():
+    """Half of 4 M elements: the count lies within six standard deviations; calls and seeds give other masks."""
+    torch = _torch()
+    x = torch.ones(2048, 2048, device="cuda", dtype=torch.bfloat16)
+    outs = []
+    for seed, call in ((1, 0), (1, 1), (2, 0)):
+        y = torch.empty_like(x)
+        gpu.dropout(x, None, y, 0.5, seed, call)
+        n = int((y != 0).sum())
+        assert abs(n - 2 ** 21) <= 6 * 1024
+        outs.append(y != 0)
+    for a, b in ((0, 1), (0, 2), (1, 2)):
+        assert abs(int((outs[a] == outs[b]).sum()) - 2 ** 21) <= 6 * 1024
+
+
+def test_dropout_of_more_than_2_32_elements():
+    torch = _torch()
+    rows, cols, p, seed, call = 70000, 65528, 0.5, 11, 3
+    x = torch.ones(rows, cols, device="cuda", dtype=torch.bfloat16)
+    gpu.dropout(x, None, x, p, seed, call)
+    blk = np.arange(cols // 8)
+    for r in (0, 1, 65535, 65536, rows - 1):
+        w = philox.philox4x32_10_blocks(blk, np.full(blk.size, r), np.full(blk.size, 2), np.full(blk.size, call), philox.seed_key(seed))
+        half = np.stack([w & 0xFFFF, w >> 16], axis=-1).reshape(cols)
+        assert np.array_equal((x[r] != 0).cpu().numpy(), half >= 32768)
+    del x
+    torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------------------------------------ group norm
+
+def maps(N, P, C, dtype, pad_p=0, pad_s=0, offset=0, values=None):
+    """Maps [N, P, C] with pitches C + pad_p and P (C + pad_p) + pad_s inside a buffer of NaN; (buffer, view, mask of what is not ours)."""
+    torch = _torch()
+    sp, ss = C + pad_p, P * (C + pad_p) + pad_s
+    buf = torch.full((offset + N * ss + 16,), float("nan"), dtype=dtype, device="cuda")
+    view = buf.as_strided((N, P, C), (ss, sp, 1), offset)
+    if values is not None:
+        view.copy_(values)
+    outside = torch.ones_like(buf, dtype=torch.bool)
+    outside.as_strided((N, P, C), (ss, sp, 1), offset).fill_(False)
+    return buf, view, outside
+
+
+def chain(n):
+    """Longest run of additions in a sum of n terms: at most n / 64 per thread and 64 in the tree above them."""
+    return 64 + n / 64
+
+
+def norm_parts(x64, G, eps):
+    N, P, C = x64.shape
+    xg = x64.view(N, P, G, C // G)
+    mean = xg.mean(dim=(1, 3))
+    var = ((xg - mean[:, None, :, None]) ** 2).mean(dim=(1, 3))
+    return xg, mean, var, 1 / (var + eps).sqrt()
+
+
+def norm_case(N, P, C, G, bf16, act, affine=True, pad_p=0, pad_s=0, offset=0, seed=0, shift=0.5, eps=1e-5, stats=True, in_place=False):
+    torch = _torch()
+    g = gen(seed)
+    d, u = dt(bf16), half_step(bf16)
+    _, x, _ = maps(N, P, C, d, pad_p, pad_s, offset, (randn(g, N, P, C) + shift * randn(g, C)).to(d))
+    x64 = x.double().clone()
+    buf, y, outside = (None, x, None) if in_place else maps(N, P, C, d, pad_p, pad_s, offset)
+    w = (1 + 0.2 * randn(g, C)).to(d) if affine else None
+    b = randn(g, C, scale=0.3, dtype=d) if affine else None
+    mean = torch.full((N, G), float("nan"), device="cuda") if stats else None
+    rstd = torch.full((N, G), float("nan"), device="cuda") if stats else None
+    gpu.group_norm(x, G, w, b, y, mean, rstd, eps, act)
+    torch.cuda.synchronize()
+    xg, m64, v64, r64 = norm_parts(x64, G, eps)
+    n = P * (C // G)
+    # mean: n additions in chains, a division; variance: deviations from the computed mean (its error enters squared)
+    tm = (chain(n) + 4) * 2.0 ** -24 * xg.abs().mean(dim=(1, 3))
+    tv = (chain(n) + 8) * 2.0 ** -23 * v64 + tm ** 2 + 2 * tm * 2.0 ** -23 * v64.sqrt()
+    tr = r64 * (0.5 * tv / (v64 + eps) + 2.0 ** -22)
+    if stats:
+        within(mean, m64, tm)
+        within(rstd, r64, tr)
+    e = lambda t: t[:, None, :, None]                                     # noqa: E731
+    xh = (xg - e(m64)) * e(r64)
+    txh = e(tm) * e(r64) + (xg - e(m64)).abs() * e(tr) + 2.0 ** -22 * xh.abs()
+    w64 = w.double().view(G, C // G) if affine else 1.0
+    b64 = b.double().view(G, C // G) if affine else 0.0
+    z = xh * w64 + b64
+    tz = txh * (w64.abs() if affine else 1.0) + 2.0 ** -23 * (z.abs() + (b64.abs() if affine else 0.0))
+    want = act64(z, act)
+    tol = u * want.abs() + 1.2 * tz + (E20 * (1 + z.abs()) if smooth(act) else 0.0) + E23 * want.abs()
+    within(y, want.view(N, P, C), tol.view(N, P, C))
+    if not in_place:
+        assert bool(torch.isnan(buf[outside]).all())
+
+
+NORM_SIZES = [
+    (1, 1, 1, 1), (2, 1, 6, 3), (3, 49, 7, 7), (5, 13, 64, 64), (4, 196, 6, 2), (20, 784, 6, 3), (3, 100, 16, 1), (2, 1024, 64, 8), (2, 255, 320, 32),
+    (7, 81, 84, 7), (2, 4096, 32, 4), (1, 20000, 8, 2), (1, 9000, 96, 3), (3, 16, 1000, 10), (2, 5, 4099, 1), (2, 30, 8200, 2), (1, 70000, 20, 4),
+    (64, 64, 128, 32), (2, 3000, 512, 4)]
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("N,P,C,G", NORM_SIZES)
+def test_group_norm_sizes(N, P, C, G, bf16):
+    norm_case(N, P, C, G, bf16, gpu.ACT_SILU, seed=N + P + C)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("affine", [False, True])
+def test_group_norm_epilogues(act, affine, bf16):
+    norm_case(3, 144, 48, 6, bf16, act, affine, seed=act, stats=affine)
+    norm_case(3, 50, 21, 3, bf16, act, affine, seed=act, in_place=True)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("pad_p,pad_s,offset", [(8, 0, 0), (0, 24, 8), (1, 0, 0), (0, 1, 0), (0, 0, 1), (3, 5, 7), (4, 4, 4)])
+def test_group_norm_pitches_and_alignment(pad_p, pad_s, offset, bf16):
+    for C, G in ((64, 8), (24, 8), (10, 5)):
+        norm_case(3, 120, C, G, bf16, gpu.ACT_RELU, pad_p=pad_p, pad_s=pad_s, offset=offset, seed=offset)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_group_norm_far_from_zero(bf16):
+    """Means 300 standard deviations away: the variance is that of the deviations."""
+    norm_case(2, 400, 32, 4, bf16, gpu.ACT_NONE, shift=300.0, seed=2)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_group_norm_of_constant_groups(bf16):
+    """No variance: y = act(b), rstd = 1 / sqrt(eps)."""
+    torch = _torch()
+    d = dt(bf16)
+    x = torch.full((2, 9, 16), 3.0, device="cuda", dtype=d)
+    b = torch.arange(16, device="cuda").to(d)
+    y = torch.empty_like(x)
+    mean, rstd = torch.empty(2, 4, device="cuda"), torch.empty(2, 4, device="cuda")
+    gpu.group_norm(x, 4, None, b, y, mean, rstd, 1e-4)
+    assert torch.equal(y, b.expand(2, 9, 16)) and torch.equal(mean, torch.full_like(mean, 3.0))
+    within(rstd, torch.full_like(rstd, 100.0).double(), 100 * 2.0 ** -22)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_group_norm_keeps_nan_in_its_group(bf16):
+    torch = _torch()
+    d = dt(bf16)
+    for P in (10, 5000):
+        x = randn(gen(1), 3, P, 32, dtype=d)
+        x[1, 4, 9] = float("nan")
+        y = torch.empty_like(x)
+        gpu.group_norm(x, 4, None, None, y, None, None)
+        bad = torch.isnan(y)
+        assert bool(bad[1, :, 8:16].all()) and int(bad.sum()) == P * 8
+
+
+def norm_grad_case(N, P, C, G, bf16, act, affine=True, pad_p=0, pad_s=0, offset=0, seed=0, want=(True, True, True), in_place=False, differences=False):
+    torch = _torch()
+    g = gen(seed)
+    d, u = dt(bf16), half_step(bf16)
+    eps = 1e-5
+    _, x, _ = maps(N, P, C, d, pad_p, pad_s, offset, (randn(g, N, P, C) + 0.5 * randn(g, C)).to(d))
+    _, dy, _ = maps(N, P, C, d, pad_p, pad_s, offset, randn(g, N, P, C, dtype=d))
+    x64, dy64 = x.double(), dy.double().clone()
+    w = (1 + 0.2 * randn(g, C)).to(d) if affine else None
+    b = randn(g, C, scale=0.3, dtype=d) if affine else None
+    _, m64, _, r64 = norm_parts(x64, G, eps)
+    mean, rstd = m64.float().contiguous(), r64.float().contiguous()
+    buf, dx, outside = maps(N, P, C, d, pad_p, pad_s, offset)
+    if in_place:
+        dx = dy
+    dw = torch.full((C,), float("nan"), device="cuda", dtype=d) if want[1] else None
+    db = torch.full((C,), float("nan"), device="cuda", dtype=d) if want[2] else None
+    gpu.group_norm_grad(dy, x, G, w, b, mean, rstd, dx if want[0] else None, dw, db, act)
+    torch.cuda.synchronize()
+    e = lambda t: t.double()[:, None, :, None]                            # noqa: E731
+    xg, gy = x64.view(N, P, G, C // G), dy64.view(N, P, G, C // G)
+    xh = (xg - e(mean)) * e(rstd)
+    w64 = w.double().view(G, C // G) if affine else torch.ones(G, C // G, dtype=torch.float64, device="cuda")
+    b64 = b.double().view(G, C // G) if affine else torch.zeros(G, C // G, dtype=torch.float64, device="cuda")
+    z = xh * w64 + b64
+    txh = 2.0 ** -22 * xh.abs()
+    tz = txh * w64.abs() + 2.0 ** -23 * (z.abs() + b64.abs())
+    gz = gy * slope64(z, act)
+    tg = 2.0 ** -23 * gz.abs() + (gy.abs() * (0.8 * tz + E20 * (1 + z.abs())) if smooth(act) else 0.0)
+    n = P * (C // G)
+    if want[1]:
+        s = (gz * xh).sum(dim=(0, 1))
+        tol = (tg * xh.abs() + gz.abs() * txh + (chain(N * P) + 8) * 2.0 ** -23 * (gz * xh).abs()).sum(dim=(0, 1))
+        within(dw, s.reshape(C), (u * s.abs() + tol).reshape(C))
+    if want[2]:
+        s = gz.sum(dim=(0, 1))
+        within(db, s.reshape(C), (u * s.abs() + (tg + (chain(N * P) + 8) * 2.0 ** -23 * gz.abs()).sum(dim=(0, 1))).reshape(C))
+    if want[0]:
+        gw, tgw = gz * w64, tg * w64.abs() + 2.0 ** -23 * (gz * w64).abs()
+        mean_of = lambda t: t.mean(dim=(1, 3), keepdim=True)              # noqa: E731
+        s1, s2 = mean_of(gw), mean_of(gw * xh)
+        L = (chain(n) + 8) * 2.0 ** -23
+        t1 = mean_of(tgw) + L * mean_of(gw.abs())
+        t2 = mean_of(tgw * xh.abs() + gw.abs() * txh) + L * mean_of((gw * xh).abs())
+        out = e(rstd) * (gw - s1 - xh * s2)
+        tol = u * out.abs() + e(rstd) * (tgw + t1 + xh.abs() * t2 + txh * s2.abs() + 2.0 ** -22 * (gw.abs() + s1.abs() + (xh * s2).abs()))
+        within(dx, out.view(N, P, C), tol.view(N, P, C))
+        if not in_place:
+            assert bool(torch.isnan(buf[outside]).all())
+    if differences:
+        # L = sum dy act(group_norm(x) w + b) in 64 bits, central differences of step 1e-6 (truncation 1e-10 or less); the gradients
+        # are taken at mean and rstd rounded to fp32 (2^-24 each), which moves xh by 2^-23 (|xh| + |mean| rstd)
+        h = 1e-6
+
+        def loss(xx, ww, bb):
+            q, m, _, r = norm_parts(xx, G, eps)
+            return float((gy * act64((q - m[:, None, :, None]) * r[:, None, :, None] * ww + bb, act)).sum())
+
+        for got, at in ((dx, 0), (dw, 1), (db, 2)):
+            args = [x64.contiguous(), w64, b64]
+            v = torch.randn(args[at].shape, generator=g, device="cuda", dtype=torch.float64)
+            lo, hi = list(args), list(args)
+            lo[at], hi[at] = args[at] - h * v, args[at] + h * v
+            num = (loss(*hi) - loss(*lo)) / (2 * h)
+            mag = float((got.double().reshape(v.shape).abs() * v.abs()).sum())
+            assert abs(float((got.double().reshape(v.shape) * v).sum()) - num) <= 1e-5 * mag + 1e-6
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("N,P,C,G", NORM_SIZES)
+def test_group_norm_grad_sizes(N, P, C, G, bf16):
+    norm_grad_case(N, P, C, G, bf16, gpu.ACT_SILU, seed=N + P + C)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("affine", [False, True])
+def test_group_norm_grad_epilogues(act, affine, bf16):
+    norm_grad_case(3, 144, 48, 6, bf16, act, affine, seed=act)
+    norm_grad_case(3, 50, 21, 3, bf16, act, affine, seed=act, in_place=True)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("want", [(True, False, False), (False, True, False), (False, False, True), (False, True, True)])
+def test_group_norm_grad_of_chosen_operands(want, bf16):
+    norm_grad_case(3, 144, 48, 6, bf16, gpu.ACT_GELU, seed=1, want=want)
+    norm_grad_case(2, 3000, 48, 6, bf16, gpu.ACT_GELU, seed=1, want=want)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("pad_p,pad_s,offset", [(8, 0, 0), (0, 24, 8), (1, 0, 0), (0, 1, 0), (0, 0, 1), (3, 5, 7), (4, 4, 4)])
+def test_group_norm_grad_pitches_and_alignment(pad_p, pad_s, offset, bf16):
+    for C, G in ((64, 8), (24, 8), (10, 5)):
+        norm_grad_case(3, 120, C, G, bf16, gpu.ACT_RELU, pad_p=pad_p, pad_s=pad_s, offset=offset, seed=offset)
+
+
+@pytest.mark.parametrize("act", [gpu.ACT_NONE, gpu.ACT_GELU, gpu.ACT_SILU])
+def test_group_norm_grad_against_differences(act):
+    norm_grad_case(3, 40, 24, 4, False, act, seed=9, differences=True)
+
+
+def test_group_norm_of_images_and_without_samples():
+    """[N, H, W, C] maps, also as a crop of larger images whose rows are not at one pitch (refused) and at one pitch (taken)."""
+    torch = _torch()
+    x = randn(gen(4), 2, 8, 8, 16)
+    y = torch.empty_like(x)
+    gpu.group_norm(x, 4, None, None, y, None, None)
+    flat = torch.empty(2, 64, 16, device="cuda")
+    gpu.group_norm(x.view(2, 64, 16), 4, None, None, flat, None, None)
+    assert torch.equal(y.view(2, 64, 16), flat)
+    with pytest.raises(ValueError):
+        gpu.group_norm(x[:, :, :5], 4, None, None, y[:, :, :5], None, None)
+    crop = torch.empty(2, 5, 8, 16, device="cuda")
+    gpu.group_norm(x[:, :5], 4, None, None, crop, None, None)
+    want = torch.empty(2, 5, 8, 16, device="cuda")
+    gpu.group_norm(x[:, :5].contiguous(), 4, None, None, want, None, None)
+    assert torch.equal(crop, want)
+    empty = torch.empty(0, 8, 8, 16, device="cuda")
+    gpu.group_norm(empty, 4, None, None, empty.clone(), None, None)
+    dw = torch.ones(16, device="cuda")
+    st = torch.empty(0, 4, device="cuda")
+    gpu.group_norm_grad(empty, empty.clone(), 4, None, None, st, st.clone(), empty.clone(), dw, None)
+    assert float(dw.abs().sum()) == 0.0
+
+
+# ------------------------------------------------------------------------------------------------ together, streams, graphs
+
+class Block:
+    """A residual block of channels-last maps x [N, P, C]: y = x + dropout(gelu(silu(group_norm(x)) W1 + b1)) W2 + b2, forward and
+    backward through the operations, all buffers its own."""
+
+    def __init__(self, N, P, C, H, bf16, seed):
+        torch = _torch()
+        g, d = gen(seed), dt(bf16)
+        self.N, self.P, self.C, self.H, self.p, self.seed, self.call = N, P, C, H, 0.25, 77, 5
+        self.x, self.dy = randn(g, N, P, C, dtype=d), randn(g, N, P, C, dtype=d)
+        self.gw, self.gb = (1 + 0.1 * randn(g, C)).to(d), randn(g, C, scale=0.1, dtype=d)
+        self.w1, self.b1 = randn(g, C, H, scale=math.sqrt(2 / C), dtype=d), randn(g, H, scale=0.1, dtype=d)
+        self.w2, self.b2 = randn(g, H, C, scale=math.sqrt(2 / H), dtype=d), randn(g, C, scale=0.1, dtype=d)
+        e = lambda *s: torch.zeros(*s, device="cuda", dtype=d)            # noqa: E731
+        self.h, self.z, self.a, self.q, self.y = e(N, P, C), e(N * P, H), e(N * P, H), e(N * P, H), e(N, P, C)
+        self.mean, self.rstd = torch.zeros(N, 4, device="cuda"), torch.zeros(N, 4, device="cuda")
+        self.dq, self.da, self.dh, self.dx = e(N * P, H), e(N * P, H), e(N, P, C), e(N, P, C)
+        self.dw1, self.db1, self.dw2, self.db2, self.dgw, self.dgb = e(C, H), e(H), e(H, C), e(C), e(C), e(C)
+        code = gpu.BF16_FP32MASTER if bf16 else gpu.FP32
+        need = [gpu.linear_scratch_bytes(N * P, C, H, gpu.ACT_GELU, code, grad) for grad in (False, True)]
+        need += [gpu.linear_scratch_bytes(N * P, H, C, gpu.ACT_NONE, code, grad) for grad in (False, True)]
+        need += [gpu.group_norm_scratch_bytes(N, P, C, 4, code, grad) for grad in (False, True)]
+        self.scratch = torch.empty(max(need) + 1, dtype=torch.uint8, device="cuda")
+
+    def step(self, stream=None):
+        N, P, C = self.N, self.P, self.C
+        rows = lambda t: t.view(N * P, C)                                 # noqa: E731
+        kw = dict(scratch=self.scratch, stream=stream)
+        gpu.group_norm(self.x, 4, self.gw, self.gb, self.h, self.mean, self.rstd, 1e-5, gpu.ACT_SILU, **kw)
+        gpu.linear(rows(self.h), self.w1, self.b1, None, self.a, gpu.ACT_GELU, pre=self.z, **kw)
+        gpu.dropout(self.a, None, self.q, self.p, self.seed, self.call, stream=stream)
+        gpu.linear(self.q, self.w2, self.b2, rows(self.x), rows(self.y), **kw)
+        gpu.linear_grad(rows(self.dy), self.q, self.w2, None, self.dq, self.dw2, self.db2, **kw)
+        gpu.dropout(self.dq, None, self.da, self.p, self.seed, self.call, stream=stream)
+        gpu.linear_grad(self.da, rows(self.h), self.w1, self.z, rows(self.dh), self.dw1, self.db1, gpu.ACT_GELU, **kw)
+        gpu.group_norm_grad(self.dh, self.x, 4, self.gw, self.gb, self.mean, self.rstd, self.dx, self.dgw, self.dgb, gpu.ACT_SILU, **kw)
+
+    def results(self):
+        """(dx is the branch's part: the residual path adds dy)"""
+        return [t.clone() for t in (self.y, self.dx, self.dgw, self.dgb, self.dw1, self.db1, self.dw2, self.db2)]
+
+    def reference(self):
+        torch = _torch()
+        N, P, C, G = self.N, self.P, self.C, 4
+        leaves = [t.double().requires_grad_() for t in (self.x, self.gw, self.gb, self.w1, self.b1, self.w2, self.b2)]
+        x, gw, gb, w1, b1, w2, b2 = leaves
+        keep = torch.from_numpy(keep_mask(N * P, self.H, self.p, self.seed, self.call)).cuda()
+        xg, m, _, r = norm_parts(x, G, 1e-5)
+        u = ((xg - m[:, None, :, None]) * r[:, None, :, None]).reshape(N * P, C) * gw + gb
+        a = act64(act64(u, gpu.ACT_SILU) @ w1 + b1, gpu.ACT_GELU)
+        branch = (keep * a * (65536 / (65536 - 16384))) @ w2 + b2
+        grads = torch.autograd.grad((branch * self.dy.double().view(N * P, C)).sum(), leaves)
+        return [(branch + x.view(N * P, C)).view(N, P, C).detach(), grads[0]] + list(grads[1:])
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("N,P,C,H", [(3, 49, 32, 64), (2, 100, 36, 75), (4, 256, 128, 256)])
+def test_a_residual_block_forward_and_backward(N, P, C, H, bf16):
+    """Relative to each result's norm: six stored quantities lie between the inputs and the last gradient, each rounded by at most half
+    a step u; the products' sums in fp32 add (C + H) 2^-23.  Independent errors at most add up: 8 u."""
+    block = Block(N, P, C, H, bf16, 1)
+    block.step()
+    tol = 8 * half_step(bf16) + 4 * (C + H) * E23
+    for got, want in zip(block.results(), block.reference()):
+        assert float((got.double().view(want.shape) - want).norm()) <= tol * float(want.norm())
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_captured_steps_and_other_streams_give_the_same_bits(bf16):
+    torch = _torch()
+    one = Block(4, 100, 64, 128, bf16, 2)
+    one.step()
+    torch.cuda.synchronize()
+    want = one.results()
+    one.step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(one.results(), want))
+    # two steps at once on streams of their own
+    two, three = Block(4, 100, 64, 128, bf16, 2), Block(4, 100, 64, 128, bf16, 2)
+    s2, s3 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        two.step(stream=s2)
+        three.step(stream=s3)
+    torch.cuda.synchronize()
+    for blk in (two, three):
+        assert all(torch.equal(a, b) for a, b in zip(blk.results(), want))
+    # captured, then replayed on new inputs
+    four = Block(4, 100, 64, 128, bf16, 3)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        four.step()
+    four.x.copy_(one.x)
+    four.dy.copy_(one.dy)
+    for name in ("gw", "gb", "w1", "b1", "w2", "b2"):
+        getattr(four, name).copy_(getattr(one, name))
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(four.results(), want))
+
+
+def test_scratch_allocated_by_the_call_on_another_stream():
+    torch = _torch()
+    g = gen(6)
+    dy, x, w, z = randn(g, 500, 129), randn(g, 500, 65), randn(g, 65, 129), randn(g, 500, 129)
+    outs = []
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (None, s):
+        dx, dw, db = torch.empty(500, 65, device="cuda"), torch.empty(65, 129, device="cuda"), torch.empty(129, device="cuda")
+        torch.cuda.synchronize()
+        for _ in range(4):
+            gpu.linear_grad(dy, x, w, z, dx, dw, db, gpu.ACT_GELU, stream=stream)
+        torch.cuda.synchronize()
+        outs.append((dx, dw, db))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def test_layer_operations_refuse_wrong_tensors():
+    torch = _torch()
+    x, w, y = torch.zeros(4, 8, device="cuda"), torch.zeros(8, 16, device="cuda"), torch.zeros(4, 16, device="cuda")
+    with pytest.raises(ValueError):
+        gpu.linear(x.double(), w, None, None, y)
+    with pytest.raises(ValueError):
+        gpu.linear(x, w.bfloat16(), None, None, y)
+    with pytest.raises(ValueError):
+        gpu.linear(x, w, None, None, y[:3])
+    with pytest.raises(ValueError):
+        gpu.linear(x, w, None, None, torch.zeros(16, 4, device="cuda").t())
+    with pytest.raises(ValueError):
+        gpu.linear(x, w.cpu(), None, None, y)
+    with pytest.raises(gpu.AbsError) as e:
+        gpu.linear(x, w, None, None, y.as_strided((4, 16), (8, 1)))
+    assert e.value.code == gpu.EINVAL
+    with pytest.raises(gpu.AbsError) as e:
+        gpu.linear_grad(y, x, w, None, torch.empty_like(x), None, torch.empty(16, device="cuda"),
+                        scratch=torch.empty(8, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == gpu.ENOSPACE
+    with pytest.raises(gpu.AbsError) as e:
+        gpu.linear(x, w, None, None, y, 9)
+    assert e.value.code == gpu.EUNSUPPORTED
+    with pytest.raises(ValueError):
+        gpu.dropout(x, None, x, 0.5, 1 << 64, 0)
+    with pytest.raises(gpu.AbsError) as e:
+        gpu.dropout(x, None, x, 1.5, 0, 0)
+    assert e.value.code == gpu.EINVAL
+    m = torch.zeros(2, 9, 16, device="cuda")
+    with pytest.raises(gpu.AbsError) as e:
+        gpu.group_norm(m, 5, None, None, m, None, None)
+    assert e.value.code == gpu.EINVAL
+    with pytest.raises(ValueError):
+        gpu.group_norm(m, 4, torch.ones(8, device="cuda"), None, m, None, None)
