@@ -312,7 +312,7 @@ int abs_lsq_gradient_noalloc(const void* X, const float* y, const void* w, const
  * x [rows][n_in], w [n_in][n_out] (the parameter layout of w0 and abs_get_params), bias [n_out] or
  * NULL, residual [rows][n_out] or NULL, y [rows][n_out]; pre [rows][n_out] receives z (the backward
  * pass needs it unless act is ABS_ACT_NONE) or is NULL.  y may be the same matrix as residual.
- * rows in [0, 2^31), n_in and n_out in [1, 2^20]. */
+ * rows in [0, 2^30], n_in and n_out in [1, 2^20]. */
 int abs_linear(const void* x, long long ldx, const void* w, long long ldw, const void* bias, const void* residual,
                long long ldr, void* y, long long ldy, void* pre, long long ldp, long long rows, int n_in, int n_out,
                int act, int dtype, void* scratch, size_t scratch_bytes, void* stream);
@@ -365,6 +365,11 @@ int abs_group_norm_grad(const void* dy, long long dys, long long dyp, const void
 /* Scratch of abs_group_norm (grad = 0) or abs_group_norm_grad (grad = 1). */
 int abs_group_norm_scratch_bytes(long long samples, long long positions, int channels, int groups, int dtype, int grad,
                                  size_t* out);
+
+/* Status of the layer operations on the current device: ABS_ETIMEOUT if, since the last call of this
+ * function, a bounded wait (100 ms) inside one of their kernels ran out, whose results are then not valid; else
+ * ABS_OK.  Synchronises the stream; operations on other streams are covered once they have completed. */
+int abs_op_status(void* stream);
 
 /* How the context runs (the paper has no counterpart): *partials = number of fp32 partial sums
  * the Eq. 3 step adds up per parameter (0: one per selected worker), *row_block = padding unit of

@@ -100,6 +100,7 @@ def lib():
         l.abs_group_norm.argtypes = [p, q, q, p, p, p, q, q, p, p, q, q, i, i, C.c_float, i, i, p, z, p]
         l.abs_group_norm_grad.argtypes = [p, q, q, p, q, q, p, p, p, p, p, q, q, p, p, q, q, i, i, i, i, p, z, p]
         l.abs_group_norm_scratch_bytes.argtypes = [q, q, i, i, i, i, C.POINTER(z)]
+        l.abs_op_status.argtypes = [p]
         l.abs_get_plan.argtypes = [C.c_void_p, C.POINTER(C.c_int), C.POINTER(C.c_int),
                                    C.POINTER(C.c_int), C.POINTER(C.c_int)]
         l.abs_profile_start.argtypes = [C.c_void_p, C.c_int]
@@ -501,6 +502,13 @@ def group_norm_scratch_bytes(samples, positions, channels, groups, dtype=BF16_FP
     out = C.c_size_t(0)
     _check(lib().abs_group_norm_scratch_bytes(samples, positions, channels, groups, dtype, int(grad), C.byref(out)))
     return out.value
+
+
+def op_status(stream=None):
+    """abs_op_status on the current device: waits for `stream` (default: the current one) and raises AbsError(ETIMEOUT) if a
+    bounded wait of a layer operation ran out since the last call."""
+    s = stream if stream is not None else _torch().cuda.current_stream()
+    _check(lib().abs_op_status(s.cuda_stream))
 
 
 def _positions(shape):

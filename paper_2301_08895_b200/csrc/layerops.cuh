@@ -19,7 +19,9 @@ int current_device(int* device, int* sms);           // linear.cu
 // A kernel that uses more than 48 KB of dynamic shared memory says so once per device.
 template <typename... KArgs>
 cudaError_t allow_smem(void (*kernel)(KArgs...), size_t bytes) {
-  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e != cudaSuccess) cudaGetLastError();
+  return e;
 }
 
 // Launch that may start while the kernel in front of it drains: every kernel of these operations waits for that one
@@ -40,7 +42,9 @@ cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int threads, size_t smem
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+  if (e != cudaSuccess) cudaGetLastError();            // (reported by this call; not to be found by the caller's next one)
+  return e;
 }
 
 // ---- device memory of a matrix: rows of `cols` elements, `ld` apart

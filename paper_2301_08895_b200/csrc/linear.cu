@@ -4,6 +4,7 @@
 #include <cstdio>
 
 #include "layerops.cuh"
+#include "linear_tc.cuh"
 
 using namespace absb;
 using namespace absb::layer;
@@ -40,6 +41,8 @@ int current_device(int* device, int* sms) {
 }  // namespace absb
 
 namespace {
+
+constexpr int BK_TERMS = tc::BK;
 
 // C[i][j] = sum_k A(i, k) B(k, j) on FP32 FMAs; A and B by element strides, so that the three products of the layer are one kernel.
 struct ProdArgs {
@@ -91,7 +94,7 @@ __global__ void __launch_bounds__(256) product_kernel(ProdArgs p) {
 
 // dz = dy act'(pre), rounded to storage, and the column sums of the unrounded dz over each block of rows
 template <typename T, int ACT>
-__global__ void __launch_bounds__(256) slope_kernel(const void* dy, long long lddy, const void* pre, long long ldp, void* dz, float* part,
+__global__ void __launch_bounds__(256) slope_kernel(const void* dy, long long lddy, const void* pre, long long ldp, void* dz, long long lddz, float* part,
                                                     long long rows, int n, int chunk) {
   grid_dependency_sync();
   __shared__ float red[8][33];
@@ -101,10 +104,8 @@ __global__ void __launch_bounds__(256) slope_kernel(const void* dy, long long ld
   if (j < n)
     for (long long m = m0 + r; m < m1; m += 8) {
       float g = ldf((const T*)dy, m * lddy + j);
-      if (ACT != ABS_ACT_NONE) {
-        g *= act_slope<ACT>(ldf((const T*)pre, m * ldp + j));
-        stf((T*)dz, m * n + j, g);
-      }
+      if (ACT != ABS_ACT_NONE) g *= act_slope<ACT>(ldf((const T*)pre, m * ldp + j));
+      if (dz) stf((T*)dz, m * lddz + j, g);
       s += g;
     }
   red[r][lane] = s;
@@ -126,27 +127,246 @@ __global__ void __launch_bounds__(256) column_kernel(const float* part, int chun
   stf((T*)db, j, t);
 }
 
+// Partial results of a split sum: C = epilogue(sum over splits), in order.
+struct FinishArgs {
+  const float* part;
+  int splits, I, J, Jp;                  // Jp: pitch of a partial row
+  const __nv_bfloat16* bias; const __nv_bfloat16* res; __nv_bfloat16* out; __nv_bfloat16* pre;
+  long long ldr, ldo, ldp;
+  Divisor quads;                         // groups of four columns per row
+  uint32_t n;                            // groups
+};
+template <int ACT>
+__global__ void __launch_bounds__(256) finish_kernel(FinishArgs a) {
+  grid_dependency_sync();
+  for (uint32_t q = blockIdx.x * 256u + threadIdx.x; q < a.n; q += gridDim.x * 256u) {
+    const uint32_t i = a.quads.div(q), j = 4u * (q - i * a.quads.d);
+    const float* p = a.part + (size_t)i * a.Jp + j;
+    const size_t step = (size_t)a.I * a.Jp;
+    float4 s = *reinterpret_cast<const float4*>(p);
+#pragma unroll 4
+    for (int k = 1; k < a.splits; ++k) {
+      const float4 t = *reinterpret_cast<const float4*>(p + k * step);
+      s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+    }
+    const float z[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if ((int)j + e >= a.J) break;
+      const float v = z[e] + (a.bias ? __bfloat162float(a.bias[j + e]) : 0.f);
+      if (a.pre) a.pre[(long long)i * a.ldp + j + e] = __float2bfloat16_rn(v);
+      float y = act_value<ACT>(v);
+      if (a.res) y += __bfloat162float(a.res[(long long)i * a.ldr + j + e]);
+      a.out[(long long)i * a.ldo + j + e] = __float2bfloat16_rn(y);
+    }
+  }
+}
+
+// Copy of a matrix with a row pitch that TMA can address (a multiple of eight elements, the start on 16 bytes).
+__global__ void __launch_bounds__(256) pack_kernel(const __nv_bfloat16* src, long long ld, long long rows, int cols, __nv_bfloat16* dst, int pitch) {
+  grid_dependency_sync();
+  const int per = pitch / 8;
+  const long long n = rows * per;
+  for (long long u = blockIdx.x * 256ll + threadIdx.x; u < n; u += gridDim.x * 256ll) {
+    const long long r = u / per;
+    const int c = (int)(u - r * per) * 8;
+    const __nv_bfloat16* s = src + r * ld + c;
+    __nv_bfloat16 v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? s[e] : __float2bfloat16_rn(0.f);
+    *reinterpret_cast<uint4*>(dst + r * pitch + c) = *reinterpret_cast<const uint4*>(v);
+  }
+}
+
 typedef void (*ProdFn)(ProdArgs);
 template <typename T> ProdFn product_fn(int act) {
   return act == ABS_ACT_RELU ? (ProdFn)product_kernel<T, ABS_ACT_RELU> : act == ABS_ACT_GELU ? (ProdFn)product_kernel<T, ABS_ACT_GELU>
          : act == ABS_ACT_SILU ? (ProdFn)product_kernel<T, ABS_ACT_SILU> : (ProdFn)product_kernel<T, ABS_ACT_NONE>;
 }
-typedef void (*SlopeFn)(const void*, long long, const void*, long long, void*, float*, long long, int, int);
+typedef void (*SlopeFn)(const void*, long long, const void*, long long, void*, long long, float*, long long, int, int);
 template <typename T> SlopeFn slope_fn(int act) {
   return act == ABS_ACT_RELU ? (SlopeFn)slope_kernel<T, ABS_ACT_RELU> : act == ABS_ACT_GELU ? (SlopeFn)slope_kernel<T, ABS_ACT_GELU>
          : act == ABS_ACT_SILU ? (SlopeFn)slope_kernel<T, ABS_ACT_SILU> : (SlopeFn)slope_kernel<T, ABS_ACT_NONE>;
 }
+typedef void (*FinishFn)(FinishArgs);
+FinishFn finish_fn(int act) {
+  return act == ABS_ACT_RELU ? (FinishFn)finish_kernel<ABS_ACT_RELU> : act == ABS_ACT_GELU ? (FinishFn)finish_kernel<ABS_ACT_GELU>
+         : act == ABS_ACT_SILU ? (FinishFn)finish_kernel<ABS_ACT_SILU> : (FinishFn)finish_kernel<ABS_ACT_NONE>;
+}
 
-int run_product(const ProdArgs& p, int act, int dtype, cudaStream_t s) {
+size_t round256(size_t v) { return (v + 255) / 256 * 256; }
+
+// ------------------------------------------------------------------ tensor-core products (bf16)
+
+// How a product C[I][J] = sum over K terms is cut up.
+struct Plan { int bn, cg, splits, kb_per; size_t part_bytes; };
+
+// The cheapest of the four tiles and of the ways to split the sum, by a model in microseconds: a block of 64 terms of a tile,
+// the tiles a unit (CTA or CTA pair) takes in turn, a fixed part for filling the pipeline and the last tile's epilogue, and for
+// split sums the partial results' way through L2 and a second launch.
+Plan plan_product(long long I, int J, long long K) {
+  struct Opt { int bn, cg; double kb, fixed; };
+  static const Opt opts[4] = {{256, 2, 0.34, 6.0}, {256, 1, 0.36, 5.5}, {128, 1, 0.22, 4.5}, {64, 1, 0.16, 4.0}};
+  const long long n_kb = (K + BK_TERMS - 1) / BK_TERMS;
+  const long long Jp = (J + 3) / 4 * 4;
+  Plan best = {};
+  double best_t = 1e30;
+  for (const Opt& o : opts) {
+    const long long tiles = (I + 128 * o.cg - 1) / (128 * o.cg) * ((J + o.bn - 1) / o.bn);
+    const long long units = PLAN_SMS / o.cg;
+    for (int s = 1; s <= 64 && s <= n_kb; ++s) {
+      const long long per = (n_kb + s - 1) / s;
+      if (s > 1 && ((s - 1) * per >= n_kb || (size_t)s * I * Jp * 4 > (256u << 20))) continue;
+      double t = (double)((tiles * s + units - 1) / units) * per * o.kb + o.fixed;
+      if (s > 1) t += 2.5 + (double)s * I * Jp * 8.0 / 6e6;
+      if (t < best_t) {
+        best_t = t;
+        best = Plan{o.bn, o.cg, s, (int)per, s > 1 ? round256((size_t)s * I * Jp * 4) : 0};
+      }
+      if (tiles * s >= 2 * units) break;
+    }
+  }
+  return best;
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_fn() {
+  static std::atomic<EncodeTiledFn> known;
+  EncodeTiledFn fn = known.load(std::memory_order_acquire);
+  if (!fn) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess) {
+      fn = (EncodeTiledFn)p;
+      known.store(fn, std::memory_order_release);
+    }
+  }
+  return fn;
+}
+// bf16 matrix [rows][cols], 128-byte swizzle, boxes of 64 columns x box_rows
+bool matrix_map(CUtensorMap* map, const void* p, long long rows, long long cols, long long ld, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, one[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// fp32 partial results [splits][I][Jp], boxes of 32 x 32
+bool partial_map(CUtensorMap* map, const void* p, int I, int J, int Jp, int splits) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)J, (cuuint64_t)I, (cuuint64_t)splits};
+  const cuuint64_t strides[2] = {(cuuint64_t)Jp * 4, (cuuint64_t)Jp * 4 * I};
+  const cuuint32_t box[3] = {32, 32, 1}, one[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool tma_able(const void* p, long long rows, long long ld) { return (uintptr_t)p % 16 == 0 && (rows == 1 || ld % 8 == 0); }
+long long tma_pitch(long long rows, long long cols, long long ld) { return rows == 1 ? (cols + 7) / 8 * 8 : ld; }
+size_t pack_bytes(long long rows, long long cols) { return round256((size_t)rows * ((cols + 7) / 8 * 8) * 2); }
+
+struct Operand { const void* p; long long rows, cols, ld; };     // a stored matrix that TMA can address
+struct Result {
+  const void* bias; const void* res; long long ldr;
+  void* out; long long ldo; void* pre; long long ldp;
+  int act;
+};
+
+template <int BN, int CG>
+cudaError_t launch_dense(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const CUtensorMap& z, const dense::Args& p, int sms, int device,
+                         cudaStream_t s) {
+  static std::atomic<uint64_t> ready;
+  auto* kernel = dense::dense_kernel<BN, CG>;
+  if (!(ready.load(std::memory_order_acquire) >> device & 1)) {
+    const cudaError_t e = allow_smem(kernel, dense::Cfg<BN, CG>::SMEM_BYTES);
+    if (e != cudaSuccess) return e;
+    ready.fetch_or(1ull << device, std::memory_order_release);
+  }
+  const int units = sms / CG < p.n_tiles ? sms / CG : p.n_tiles;
+  return launch(kernel, dim3((unsigned)(units * CG)), dense::THREADS, dense::Cfg<BN, CG>::SMEM_BYTES, CG, s, a, b, o, z, p);
+}
+
+__device__ int g_status;                 // set by a kernel whose bounded wait ran out; read and cleared by abs_op_status
+int* status_word(int device) {
+  static std::atomic<int*> known[MAX_DEVICES];
+  int* p = known[device].load(std::memory_order_acquire);
+  if (!p && cudaGetSymbolAddress((void**)&p, g_status) == cudaSuccess) known[device].store(p, std::memory_order_release);
+  return p;
+}
+
+// C[I][J] = sum_t A(i, t) B(j, t) for stored operands; a_mn / b_mn: the operand is stored [t][i] / [t][j].
+int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, int J, long long K, const Result& r, float* part, int sms, int device,
+               cudaStream_t s) {
+  const Plan pl = plan_product(I, J, K);
+  const int Jp = (J + 3) / 4 * 4;
+  dense::Args p = {};
+  p.a_mn = a_mn; p.b_mn = b_mn;
+  p.I = I; p.J = J;
+  p.n_kb = (int)((K + BK_TERMS - 1) / BK_TERMS);
+  p.splits = pl.splits; p.kb_per = pl.kb_per;
+  p.n_it = (I + 128 * pl.cg - 1) / (128 * pl.cg);
+  p.n_jt = (J + pl.bn - 1) / pl.bn;
+  const long long n_tiles = (long long)p.n_it * p.n_jt * pl.splits;
+  if (n_tiles > 0x7fffffff) return fail(ABS_EUNSUPPORTED, "%lld tiles in one product", n_tiles);
+  p.n_tiles = (int)n_tiles;
+  p.status = status_word(device);
+  if (!p.status) return fail(ABS_ECUDA, "cudaGetSymbolAddress(status) failed");
+  CUtensorMap ma, mb, mo, mz;
+  bool ok = matrix_map(&ma, a.p, a.rows, a.cols, a.ld, a_mn ? 64 : 128) && matrix_map(&mb, b.p, b.rows, b.cols, b.ld, b_mn ? 64 : pl.bn / pl.cg);
+  if (pl.splits > 1) {
+    p.partial = 1;
+    ok = ok && partial_map(&mo, part, I, J, Jp, pl.splits);
+  } else {
+    p.bias = (const __nv_bfloat16*)r.bias; p.res = (const __nv_bfloat16*)r.res; p.out = (__nv_bfloat16*)r.out; p.pre = (__nv_bfloat16*)r.pre;
+    p.ldr = r.ldr; p.ldo = r.ldo; p.ldp = r.ldp;
+    p.act = r.act;
+    p.res_vec = r.res && (uintptr_t)r.res % 16 == 0 && (r.ldr % 8 == 0 || I == 1);
+    p.bias_vec = r.bias && (uintptr_t)r.bias % 16 == 0;
+    p.out_tma = tma_able(r.out, I, r.ldo);
+    p.pre_tma = r.pre && tma_able(r.pre, I, r.ldp);
+    mo = ma;
+    if (p.out_tma) ok = ok && matrix_map(&mo, r.out, I, J, tma_pitch(I, J, r.ldo), 32);
+  }
+  mz = mo;
+  if (p.pre_tma) ok = ok && matrix_map(&mz, r.pre, I, J, tma_pitch(I, J, r.ldp), 32);
+  if (!ok) return fail(ABS_ECUDA, "cuTensorMapEncodeTiled failed");
+  cudaError_t e = pl.cg == 2 ? launch_dense<256, 2>(ma, mb, mo, mz, p, sms, device, s) : pl.bn == 256 ? launch_dense<256, 1>(ma, mb, mo, mz, p, sms, device, s)
+                  : pl.bn == 128 ? launch_dense<128, 1>(ma, mb, mo, mz, p, sms, device, s) : launch_dense<64, 1>(ma, mb, mo, mz, p, sms, device, s);
+  if (e == cudaSuccess && pl.splits > 1) {
+    FinishArgs f = {};
+    f.part = part; f.splits = pl.splits; f.I = I; f.J = J; f.Jp = Jp;
+    f.bias = (const __nv_bfloat16*)r.bias; f.res = (const __nv_bfloat16*)r.res; f.out = (__nv_bfloat16*)r.out; f.pre = (__nv_bfloat16*)r.pre;
+    f.ldr = r.ldr; f.ldo = r.ldo; f.ldp = r.ldp;
+    f.quads = Divisor((uint32_t)(Jp / 4));
+    f.n = (uint32_t)((size_t)I * (Jp / 4));              // (partial results hold at most 2^26 floats)
+    const unsigned blocks = (f.n + 255) / 256;
+    e = launch(finish_fn(r.act), dim3(blocks < 8u * sms ? blocks : 8u * sms), 256, 0, 1, s, f);
+  }
+  return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
+}
+
+int pack(const void* src, long long rows, long long cols, long long ld, void* dst, int sms, cudaStream_t s) {
+  const int pitch = (int)((cols + 7) / 8 * 8);
+  const long long blocks = (rows * (pitch / 8) + 255) / 256;
+  const cudaError_t e = launch(pack_kernel, dim3((unsigned)(blocks < 16 * sms ? blocks : 16 * sms)), 256, 0, 1, s, (const __nv_bfloat16*)src, ld, rows, (int)cols,
+                               (__nv_bfloat16*)dst, pitch);
+  return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
+}
+
+int run_product(const ProdArgs& p, int act, cudaStream_t s) {
   const dim3 grid((unsigned)((p.I + 63) / 64), (unsigned)((p.J + 63) / 64));
-  const cudaError_t e = launch(dtype == ABS_FP32 ? product_fn<float>(act) : product_fn<__nv_bfloat16>(act), grid, 256, 0, 1, s, p);
+  const cudaError_t e = launch(product_fn<float>(act), grid, 256, 0, 1, s, p);
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }
 
 int check(long long rows, int n_in, int n_out, int act, int dtype) {
   if (dtype != ABS_FP32 && dtype != ABS_BF16_FP32MASTER) return fail(ABS_EUNSUPPORTED, "unknown dtype %d", dtype);
   if (act < ABS_ACT_NONE || act > ABS_ACT_SILU) return fail(ABS_EUNSUPPORTED, "unknown activation %d", act);
-  if (rows < 0 || rows >= (1ll << 31)) return fail(ABS_EINVAL, "rows %lld outside [0, 2^31)", rows);
+  if (rows < 0 || rows > (1ll << 30)) return fail(ABS_EINVAL, "rows %lld outside [0, 2^30]", rows);
   if (n_in < 1 || n_in > (1 << 20)) return fail(ABS_EINVAL, "n_in %d outside [1, 2^20]", n_in);
   if (n_out < 1 || n_out > (1 << 20)) return fail(ABS_EINVAL, "n_out %d outside [1, 2^20]", n_out);
   return ABS_OK;
@@ -158,20 +378,42 @@ int check_matrix(const char* name, const void* p, long long rows, long long cols
   return ABS_OK;
 }
 
-size_t round256(size_t v) { return (v + 255) / 256 * 256; }
-
-struct GradPlan { size_t dz, part, total; int chunk, chunks; };
-GradPlan grad_plan(long long rows, int n_out, int act, int dtype) {
+// Scratch of a call.  need_*: the operand is copied to a pitch that TMA can address (bf16).
+struct FwdPlan { size_t x, w, part, total; };
+FwdPlan fwd_plan(long long rows, int n_in, int n_out, int dtype, bool pack_x, bool pack_w) {
+  FwdPlan f = {};
+  if (dtype == ABS_FP32) return f;
+  f.w = pack_x ? pack_bytes(rows, n_in) : 0;
+  f.part = f.w + (pack_w ? pack_bytes(n_in, n_out) : 0);
+  f.total = f.part + plan_product(rows, n_out, n_in).part_bytes;
+  return f;
+}
+struct GradPlan { size_t dz, sums, x, w, part, total; long long ld_dz; int chunk, chunks; };
+GradPlan grad_plan(long long rows, int n_in, int n_out, int dtype, bool need_dz, bool pack_x, bool pack_w) {
   GradPlan g = {};
   const size_t esz = dtype == ABS_FP32 ? 4 : 2;
   long long chunk = 64;
   while ((rows + chunk - 1) / chunk > 128) chunk *= 2;
   g.chunk = (int)chunk;
   g.chunks = (int)((rows + chunk - 1) / chunk);
-  g.dz = 0;
-  g.part = act == ABS_ACT_NONE ? 0 : round256((size_t)rows * n_out * esz);
-  g.total = g.part + round256((size_t)g.chunks * n_out * 4);
+  g.ld_dz = (n_out + 7) / 8 * 8;
+  g.sums = need_dz ? round256((size_t)rows * g.ld_dz * esz) : 0;
+  g.x = g.sums + round256((size_t)g.chunks * n_out * 4);
+  g.w = g.x + (pack_x ? pack_bytes(rows, n_in) : 0);
+  g.part = g.w + (pack_w ? pack_bytes(n_in, n_out) : 0);
+  g.total = g.part;
+  if (dtype != ABS_FP32) {
+    const size_t a = plan_product(rows, n_in, n_out).part_bytes, b = plan_product(n_in, n_out, rows).part_bytes;
+    g.total += a > b ? a : b;
+  }
   return g;
+}
+
+int check_scratch(const void* scratch, size_t have, size_t need) {
+  if (need == 0) return ABS_OK;
+  if (have < need) return fail(ABS_ENOSPACE, "scratch holds %zu bytes, %zu needed", have, need);
+  if (!scratch || (uintptr_t)scratch % 256) return fail(ABS_EINVAL, "scratch is null or not 256-byte aligned");
+  return ABS_OK;
 }
 
 }  // namespace
@@ -180,8 +422,8 @@ extern "C" int abs_linear_scratch_bytes(long long rows, int n_in, int n_out, int
   if (!out) return fail(ABS_EINVAL, "out is null");
   const int rc = check(rows, n_in, n_out, act, dtype);
   if (rc != ABS_OK) return rc;
-  (void)aligned;
-  *out = grad ? grad_plan(rows, n_out, act, dtype).total : 0;
+  const bool p = dtype != ABS_FP32 && !aligned;
+  *out = rows == 0 ? 0 : grad ? grad_plan(rows, n_in, n_out, dtype, act != ABS_ACT_NONE || p, p, p).total : fwd_plan(rows, n_in, n_out, dtype, p, p).total;
   return ABS_OK;
 }
 
@@ -202,9 +444,28 @@ extern "C" int abs_linear(const void* x, long long ldx, const void* w, long long
   if (overlap(sy, sx) || overlap(sy, sw) || overlap(sy, sb)) return fail(ABS_EINVAL, "y overlaps an operand");
   if (overlap(sp, sx) || overlap(sp, sw) || overlap(sp, sb) || overlap(sp, sr) || overlap(sp, sy)) return fail(ABS_EINVAL, "pre overlaps another matrix");
   if (overlap(sy, sr) && !(y == residual && ldy == ldr)) return fail(ABS_EINVAL, "y overlaps residual without being the same matrix");
-  (void)scratch; (void)scratch_bytes;
-  const ProdArgs p = {x, w, ldx, 1, ldw, 1, rows, n_out, n_in, bias, residual, y, pre, ldr, ldy, ldp};
-  return run_product(p, act, dtype, (cudaStream_t)stream);
+  cudaStream_t s = (cudaStream_t)stream;
+  if (dtype == ABS_FP32) {
+    const ProdArgs p = {x, w, ldx, 1, ldw, 1, rows, n_out, n_in, bias, residual, y, pre, ldr, ldy, ldp};
+    return run_product(p, act, s);
+  }
+  const bool pack_x = !tma_able(x, rows, ldx), pack_w = !tma_able(w, n_in, ldw);
+  const FwdPlan f = fwd_plan(rows, n_in, n_out, dtype, pack_x, pack_w);
+  if ((rc = check_scratch(scratch, scratch_bytes, f.total)) != ABS_OK) return rc;
+  int device, sms;
+  if ((rc = current_device(&device, &sms)) != ABS_OK) return rc;
+  char* sc = (char*)scratch;
+  Operand a = {x, rows, n_in, tma_pitch(rows, n_in, ldx)}, b = {w, n_in, n_out, tma_pitch(n_in, n_out, ldw)};
+  if (pack_x) {
+    if ((rc = pack(x, rows, n_in, ldx, sc + f.x, sms, s)) != ABS_OK) return rc;
+    a.p = sc + f.x; a.ld = (n_in + 7) / 8 * 8;
+  }
+  if (pack_w) {
+    if ((rc = pack(w, n_in, n_out, ldw, sc + f.w, sms, s)) != ABS_OK) return rc;
+    b.p = sc + f.w; b.ld = (n_out + 7) / 8 * 8;
+  }
+  const Result r = {bias, residual, ldr, y, ldy, pre, ldp, act};
+  return tc_product(a, 0, b, 1, (int)rows, n_out, n_in, r, (float*)(sc + f.part), sms, device, s);
 }
 
 extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, long long ldx, const void* w, long long ldw,
@@ -236,27 +497,68 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
     for (int j = 0; j < i; ++j)
       if (overlap(outs[i], outs[j])) return fail(ABS_EINVAL, "two gradients overlap");
   }
-  const GradPlan g = grad_plan(rows, n_out, act, dtype);
-  if (scratch_bytes < g.total) return fail(ABS_ENOSPACE, "scratch holds %zu bytes, %zu needed", scratch_bytes, g.total);
-  if (!scratch || (uintptr_t)scratch % 256) return fail(ABS_EINVAL, "scratch is null or not 256-byte aligned");
-  void* dz = act == ABS_ACT_NONE ? const_cast<void*>(dy) : scratch;
-  const long long lddz = act == ABS_ACT_NONE ? lddy : n_out;
-  float* part = db ? (float*)((char*)scratch + g.part) : nullptr;
+  const bool bf16 = dtype != ABS_FP32;
+  const bool need_dz = act != ABS_ACT_NONE || (bf16 && (dx || dw) && !tma_able(dy, rows, lddy));
+  const bool pack_x = bf16 && dw && !tma_able(x, rows, ldx), pack_w = bf16 && dx && !tma_able(w, n_in, ldw);
+  const GradPlan g = grad_plan(rows, n_in, n_out, dtype, need_dz, pack_x, pack_w);
+  if ((rc = check_scratch(scratch, scratch_bytes, g.total)) != ABS_OK) return rc;
+  int device, sms;
+  if ((rc = current_device(&device, &sms)) != ABS_OK) return rc;
+  char* sc = (char*)scratch;
+  const void* dz = need_dz ? sc + g.dz : dy;
+  const long long lddz = need_dz ? g.ld_dz : lddy;
+  float* part = db ? (float*)(sc + g.sums) : nullptr;
   cudaError_t e = cudaSuccess;
-  if (act != ABS_ACT_NONE || db)
+  if (need_dz || db)
     e = launch(dtype == ABS_FP32 ? slope_fn<float>(act) : slope_fn<__nv_bfloat16>(act), dim3((unsigned)((n_out + 31) / 32), (unsigned)g.chunks), 256, 0, 1, s,
-               dy, lddy, pre, ldp, dz, part, rows, n_out, g.chunk);
+               dy, lddy, pre, ldp, need_dz ? (void*)(sc + g.dz) : (void*)nullptr, lddz, part, rows, n_out, g.chunk);
   if (db && e == cudaSuccess)
     e = launch(dtype == ABS_FP32 ? column_kernel<float> : column_kernel<__nv_bfloat16>, dim3((unsigned)((n_out + 255) / 256)), 256, 0, 1, s,
                (const float*)part, g.chunks, n_out, db);
   if (e != cudaSuccess) return fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
+  if (!bf16) {
+    if (dx) {
+      const ProdArgs p = {dz, w, lddz, 1, 1, ldw, rows, n_in, n_out, nullptr, nullptr, dx, nullptr, 0, lddx, 0};
+      if ((rc = run_product(p, ABS_ACT_NONE, s)) != ABS_OK) return rc;
+    }
+    if (dw) {
+      const ProdArgs p = {x, dz, 1, ldx, lddz, 1, n_in, n_out, rows, nullptr, nullptr, dw, nullptr, 0, lddw, 0};
+      if ((rc = run_product(p, ABS_ACT_NONE, s)) != ABS_OK) return rc;
+    }
+    return ABS_OK;
+  }
+  const Operand od = {dz, rows, n_out, tma_pitch(rows, n_out, lddz)};
+  float* split = (float*)(sc + g.part);
   if (dx) {
-    const ProdArgs p = {dz, w, lddz, 1, 1, ldw, rows, n_in, n_out, nullptr, nullptr, dx, nullptr, 0, lddx, 0};
-    if ((rc = run_product(p, ABS_ACT_NONE, dtype, s)) != ABS_OK) return rc;
+    Operand ow = {w, n_in, n_out, tma_pitch(n_in, n_out, ldw)};
+    if (pack_w) {
+      if ((rc = pack(w, n_in, n_out, ldw, sc + g.w, sms, s)) != ABS_OK) return rc;
+      ow.p = sc + g.w; ow.ld = (n_out + 7) / 8 * 8;
+    }
+    const Result r = {nullptr, nullptr, 0, dx, lddx, nullptr, 0, ABS_ACT_NONE};
+    if ((rc = tc_product(od, 0, ow, 0, (int)rows, n_in, n_out, r, split, sms, device, s)) != ABS_OK) return rc;
   }
   if (dw) {
-    const ProdArgs p = {x, dz, 1, ldx, lddz, 1, n_in, n_out, rows, nullptr, nullptr, dw, nullptr, 0, lddw, 0};
-    if ((rc = run_product(p, ABS_ACT_NONE, dtype, s)) != ABS_OK) return rc;
+    Operand ox = {x, rows, n_in, tma_pitch(rows, n_in, ldx)};
+    if (pack_x) {
+      if ((rc = pack(x, rows, n_in, ldx, sc + g.x, sms, s)) != ABS_OK) return rc;
+      ox.p = sc + g.x; ox.ld = (n_in + 7) / 8 * 8;
+    }
+    const Result r = {nullptr, nullptr, 0, dw, lddw, nullptr, 0, ABS_ACT_NONE};
+    if ((rc = tc_product(ox, 1, od, 1, n_in, n_out, rows, r, split, sms, device, s)) != ABS_OK) return rc;
   }
   return ABS_OK;
+}
+
+extern "C" int abs_op_status(void* stream) {
+  int device, sms, v = 0;
+  const int rc = current_device(&device, &sms);
+  if (rc != ABS_OK) return rc;
+  int* word = status_word(device);
+  if (!word) return fail(ABS_ECUDA, "cudaGetSymbolAddress(status) failed");
+  cudaError_t e = cudaMemcpyAsync(&v, word, sizeof v, cudaMemcpyDeviceToHost, (cudaStream_t)stream);
+  if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
+  if (e == cudaSuccess && v) e = cudaMemsetAsync(word, 0, sizeof v, (cudaStream_t)stream);
+  if (e != cudaSuccess) return fail(ABS_ECUDA, "status: %s", cudaGetErrorString(e));
+  return v ? fail(ABS_ETIMEOUT, "a bounded wait in a layer operation ran out: its results are not valid") : ABS_OK;
 }

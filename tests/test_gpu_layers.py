@@ -137,6 +137,12 @@ def test_linear_sizes(M, K, N, bf16):
     linear_case(M, K, N, bf16, gpu.ACT_SILU, True, True, seed=M + K + N + 1)
 
 
+@pytest.mark.parametrize("M,K,N", [(2300, 1000, 4096), (4224, 328, 2568), (9000, 512, 1025)])
+def test_linear_of_many_tiles(M, K, N):
+    linear_case(M, K, N, True, gpu.ACT_GELU, True, True, seed=M)
+    grad_case(M, K, N, True, gpu.ACT_GELU, seed=M)
+
+
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("residual,pre,bias", [(False, False, False), (True, False, True), (False, True, False), (True, True, True)])
