@@ -457,7 +457,7 @@ def norm_case(N, P, C, G, bf16, act, affine=True, pad_p=0, pad_s=0, offset=0, se
 NORM_SIZES = [
     (1, 1, 1, 1), (2, 1, 6, 3), (3, 49, 7, 7), (5, 13, 64, 64), (4, 196, 6, 2), (20, 784, 6, 3), (3, 100, 16, 1), (2, 1024, 64, 8), (2, 255, 320, 32),
     (7, 81, 84, 7), (2, 4096, 32, 4), (1, 20000, 8, 2), (1, 9000, 96, 3), (3, 16, 1000, 10), (2, 5, 4099, 1), (2, 30, 8200, 2), (1, 70000, 20, 4),
-    (64, 64, 128, 32), (2, 3000, 512, 4)]
+    (64, 64, 128, 32), (2, 3000, 512, 4), (1, 300000, 16, 2), (3000, 2, 8, 2), (1, 500, 8208, 3)]
 
 
 @pytest.mark.parametrize("bf16", [False, True])
