@@ -65,23 +65,166 @@ inline bool overlap(const Span& a, const Span& b) {
   return d < a.row || d + b.row > a.ld;
 }
 
-// ---- activations
-__device__ __forceinline__ float normal_cdf(float z) { return 0.5f * erfcf(-0.70710678118654752f * z); }
+// ---- activations.  Exponential and reciprocal are the hardware's approximations (2^-22 each, denormal results are zero):
+// two instructions of the special-function unit per value, where expf and a division cost some twenty instructions.
+__device__ __forceinline__ float ex2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float sigmoid(float z) { return rcp_approx(1.f + ex2_approx(-1.4426950408889634f * z)); }
+// Phi(z) and exp(-z^2 / 2): with x = |z| / sqrt(2), t = 1 / (1 + 0.3275911 x), erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2) + e,
+// |e| <= 1.5e-7 (Abramowitz and Stegun, 7.1.26); so Phi is good to 2^-23.
+__device__ __forceinline__ float normal_cdf(float z, float& bell) {
+  const float t = rcp_approx(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
+  bell = ex2_approx(-0.72134752044448170f * z * z);
+  float p = fmaf(1.061405429f, t, -1.453152027f);
+  p = fmaf(p, t, 1.421413741f);
+  p = fmaf(p, t, -0.284496736f);
+  p = fmaf(p, t, 0.254829592f);
+  const float tail = 0.5f * p * t * bell;            // Phi(-|z|)
+  return z >= 0.f ? 1.f - tail : tail;
+}
 
 template <int ACT> __device__ __forceinline__ float act_value(float z) {
   if (ACT == ABS_ACT_RELU) return fmaxf(z, 0.f);
-  if (ACT == ABS_ACT_GELU) return z * normal_cdf(z);
-  if (ACT == ABS_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
+  if (ACT == ABS_ACT_GELU) {
+    float bell;
+    return z * normal_cdf(z, bell);
+  }
+  if (ACT == ABS_ACT_SILU) return z * sigmoid(z);
   return z;
 }
 template <int ACT> __device__ __forceinline__ float act_slope(float z) {
   if (ACT == ABS_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-  if (ACT == ABS_ACT_GELU) return normal_cdf(z) + z * (0.39894228040143268f * __expf(-0.5f * z * z));
+  if (ACT == ABS_ACT_GELU) {
+    float bell;
+    const float c = normal_cdf(z, bell);
+    return fmaf(0.39894228040143268f * z, bell, c);
+  }
   if (ACT == ABS_ACT_SILU) {
-    const float s = __fdividef(1.f, 1.f + __expf(-z));
-    return s * (1.f + z * (1.f - s));
+    const float s = sigmoid(z);
+    return s * fmaf(z, 1.f - s, 1.f);
   }
   return 1.f;
+}
+
+// ---- N floats in pairs: the packed FP32 instructions of sm_100 work on two at a time
+template <int N> struct Lanes {
+  static_assert(N % 2 == 0, "pairs");
+  unsigned long long p[N / 2];
+  __device__ __forceinline__ void fill(float v) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) put(i, v, v);
+  }
+  __device__ __forceinline__ void put(int i, float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(p[i]) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ void set(const float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) put(i, v[2 * i], v[2 * i + 1]);
+  }
+  __device__ __forceinline__ void get(float (&v)[N]) const {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) asm("mov.b64 {%0, %1}, %2;" : "=f"(v[2 * i]), "=f"(v[2 * i + 1]) : "l"(p[i]));
+  }
+  // 16-byte accesses (N a multiple of four)
+  __device__ __forceinline__ void load(const float* s) {
+#pragma unroll
+    for (int i = 0; i < N / 2; i += 2) {
+      const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(s + 2 * i);
+      p[i] = q.x;
+      p[i + 1] = q.y;
+    }
+  }
+  __device__ __forceinline__ void store(float* d) const {
+#pragma unroll
+    for (int i = 0; i < N / 2; i += 2) *reinterpret_cast<ulonglong2*>(d + 2 * i) = make_ulonglong2(p[i], p[i + 1]);
+  }
+};
+template <> struct Lanes<1> {
+  float v0;
+  __device__ __forceinline__ void fill(float v) { v0 = v; }
+  __device__ __forceinline__ void set(const float (&v)[1]) { v0 = v[0]; }
+  __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = v0; }
+  __device__ __forceinline__ void load(const float* s) { v0 = *s; }
+  __device__ __forceinline__ void store(float* d) const { *d = v0; }
+};
+template <int N> __device__ __forceinline__ Lanes<N> add(const Lanes<N>& a, const Lanes<N>& b) {
+  Lanes<N> r;
+  if constexpr (N == 1) r.v0 = a.v0 + b.v0;
+  else
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.p[i]) : "l"(a.p[i]), "l"(b.p[i]));
+  return r;
+}
+template <int N> __device__ __forceinline__ Lanes<N> mul(const Lanes<N>& a, const Lanes<N>& b) {
+  Lanes<N> r;
+  if constexpr (N == 1) r.v0 = a.v0 * b.v0;
+  else
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.p[i]) : "l"(a.p[i]), "l"(b.p[i]));
+  return r;
+}
+template <int N> __device__ __forceinline__ Lanes<N> fma(const Lanes<N>& a, const Lanes<N>& b, const Lanes<N>& c) {
+  Lanes<N> r;
+  if constexpr (N == 1) r.v0 = fmaf(a.v0, b.v0, c.v0);
+  else
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.p[i]) : "l"(a.p[i]), "l"(b.p[i]), "l"(c.p[i]));
+  return r;
+}
+// 1 / (1 + exp(-z)) and so on, value by value; the products around them in pairs
+template <int ACT, int N> __device__ __forceinline__ Lanes<N> act_values(const Lanes<N>& z) {
+  if constexpr (ACT == ABS_ACT_NONE) return z;
+  float v[N];
+  Lanes<N> r;
+  if constexpr (ACT == ABS_ACT_SILU) {
+    Lanes<N> k, one;
+    k.fill(-1.4426950408889634f);
+    one.fill(1.f);
+    mul(z, k).get(v);
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = ex2_approx(v[j]);
+    r.set(v);
+    add(r, one).get(v);
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = rcp_approx(v[j]);
+    r.set(v);
+    return mul(z, r);
+  }
+  z.get(v);
+#pragma unroll
+  for (int j = 0; j < N; ++j) v[j] = act_value<ACT>(v[j]);
+  r.set(v);
+  return r;
+}
+template <int ACT, int N> __device__ __forceinline__ Lanes<N> act_slopes(const Lanes<N>& z) {
+  float v[N];
+  Lanes<N> r;
+  if constexpr (ACT == ABS_ACT_SILU) {
+    Lanes<N> k, one, minus, s;
+    k.fill(-1.4426950408889634f);
+    one.fill(1.f);
+    minus.fill(-1.f);
+    mul(z, k).get(v);
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = ex2_approx(v[j]);
+    s.set(v);
+    add(s, one).get(v);
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = rcp_approx(v[j]);
+    s.set(v);
+    return mul(s, fma(z, fma(s, minus, one), one));
+  }
+  z.get(v);
+#pragma unroll
+  for (int j = 0; j < N; ++j) v[j] = act_slope<ACT>(v[j]);
+  r.set(v);
+  return r;
 }
 
 // ---- VE consecutive stored values in one access (16 bytes, or one element), and as binary32
