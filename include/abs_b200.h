@@ -312,7 +312,8 @@ int abs_lsq_gradient_noalloc(const void* X, const float* y, const void* w, const
  * x [rows][n_in], w [n_in][n_out] (the parameter layout of w0 and abs_get_params), bias [n_out] or
  * NULL, residual [rows][n_out] or NULL, y [rows][n_out]; pre [rows][n_out] receives z (the backward
  * pass needs it unless act is ABS_ACT_NONE) or is NULL.  y may be the same matrix as residual.
- * rows in [0, 2^30], n_in and n_out in [1, 2^20]. */
+ * rows in [0, 2^30], n_in and n_out in [1, 2^20]; ABS_FP32: row pitches of x and w at most 2^24 if they have
+ * more than one row. */
 int abs_linear(const void* x, long long ldx, const void* w, long long ldw, const void* bias, const void* residual,
                long long ldr, void* y, long long ldy, void* pre, long long ldp, long long rows, int n_in, int n_out,
                int act, int dtype, void* scratch, size_t scratch_bytes, void* stream);

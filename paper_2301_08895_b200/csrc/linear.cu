@@ -5,6 +5,7 @@
 
 #include "layerops.cuh"
 #include "linear_tc.cuh"
+#include "linear_fma.cuh"
 
 using namespace absb;
 using namespace absb::layer;
@@ -43,54 +44,6 @@ int current_device(int* device, int* sms) {
 namespace {
 
 constexpr int BK_TERMS = tc::BK;
-
-// C[i][j] = sum_k A(i, k) B(k, j) on FP32 FMAs; A and B by element strides, so that the three products of the layer are one kernel.
-struct ProdArgs {
-  const void* a; const void* b;
-  long long a_i, a_k, b_k, b_j;          // element strides
-  long long I; int J; long long K;
-  const void* bias; const void* res; void* out; void* pre;
-  long long ldr, ldo, ldp;
-};
-
-template <typename T, int ACT>
-__global__ void __launch_bounds__(256) product_kernel(ProdArgs p) {
-  grid_dependency_sync();
-  __shared__ float sa[16][65], sb[16][65];
-  const long long i0 = (long long)blockIdx.x * 64;
-  const int j0 = blockIdx.y * 64;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4] = {};
-  for (long long k0 = 0; k0 < p.K; k0 += 16) {
-    for (int e = threadIdx.x; e < 1024; e += 256) {
-      const int ka = p.a_k == 1 ? e & 15 : e >> 6, ia = p.a_k == 1 ? e >> 4 : e & 63;
-      sa[ka][ia] = (i0 + ia < p.I && k0 + ka < p.K) ? ldf((const T*)p.a, (i0 + ia) * p.a_i + (k0 + ka) * p.a_k) : 0.f;
-      const int kb = p.b_k == 1 ? e & 15 : e >> 6, jb = p.b_k == 1 ? e >> 4 : e & 63;
-      sb[kb][jb] = (j0 + jb < p.J && k0 + kb < p.K) ? ldf((const T*)p.b, (k0 + kb) * p.b_k + (j0 + jb) * p.b_j) : 0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 16; ++k)
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[u][v] = fmaf(sa[k][ty + 16 * u], sb[k][tx + 16 * v], acc[u][v]);
-    __syncthreads();
-  }
-#pragma unroll
-  for (int u = 0; u < 4; ++u)
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const long long i = i0 + ty + 16 * u;
-      const int j = j0 + tx + 16 * v;
-      if (i >= p.I || j >= p.J) continue;
-      const float z = acc[u][v] + (p.bias ? ldf((const T*)p.bias, j) : 0.f);
-      if (p.pre) stf((T*)p.pre, i * p.ldp + j, z);
-      float y = act_value<ACT>(z);
-      if (p.res) y += ldf((const T*)p.res, i * p.ldr + j);
-      stf((T*)p.out, i * p.ldo + j, y);
-    }
-}
 
 // dz = dy act'(pre), rounded to storage, and the column sums of the unrounded dz over each block of rows
 template <typename T, int ACT>
@@ -178,11 +131,6 @@ __global__ void __launch_bounds__(256) pack_kernel(const __nv_bfloat16* src, lon
   }
 }
 
-typedef void (*ProdFn)(ProdArgs);
-template <typename T> ProdFn product_fn(int act) {
-  return act == ABS_ACT_RELU ? (ProdFn)product_kernel<T, ABS_ACT_RELU> : act == ABS_ACT_GELU ? (ProdFn)product_kernel<T, ABS_ACT_GELU>
-         : act == ABS_ACT_SILU ? (ProdFn)product_kernel<T, ABS_ACT_SILU> : (ProdFn)product_kernel<T, ABS_ACT_NONE>;
-}
 typedef void (*SlopeFn)(const void*, long long, const void*, long long, void*, long long, float*, long long, int, int);
 template <typename T> SlopeFn slope_fn(int act) {
   return act == ABS_ACT_RELU ? (SlopeFn)slope_kernel<T, ABS_ACT_RELU> : act == ABS_ACT_GELU ? (SlopeFn)slope_kernel<T, ABS_ACT_GELU>
@@ -357,9 +305,57 @@ int pack(const void* src, long long rows, long long cols, long long ld, void* ds
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }
 
-int run_product(const ProdArgs& p, int act, cudaStream_t s) {
-  const dim3 grid((unsigned)((p.I + 63) / 64), (unsigned)((p.J + 63) / 64));
-  const cudaError_t e = launch(product_fn<float>(act), grid, 256, 0, 1, s, p);
+// ------------------------------------------------------------------ fp32 products
+
+struct FmaPlan { int bm, Q, kb_per; };
+// 64 x 64 or 128 x 128 tiles, and how many CTAs share a tile's sum.  A block of 32 k takes a CTA that is alone on its SM 1.2 or 3.4
+// us, two of them together 2.6 or 5.8 us (4096^3: 53 TFLOP/s); joining CTAs costs about a microsecond.
+FmaPlan plan_fma(long long I, int J, int K) {
+  FmaPlan best = {};
+  double least = 1e300;
+  const int n_kb = (K + fp32::BK - 1) / fp32::BK;
+  for (int bm : {64, 128}) {
+    const long long tiles = (I + bm - 1) / bm * ((J + bm - 1) / bm);
+    const double one = bm == 64 ? 1.2 : 3.4, two = bm == 64 ? 2.6 : 5.8;
+    for (int q = 1; q <= 8 && q <= n_kb; ++q) {
+      const int per = (n_kb + q - 1) / q;
+      if ((q - 1) * per >= n_kb) continue;
+      const long long full = tiles * q / (2 * PLAN_SMS), rest = tiles * q - full * 2 * PLAN_SMS;
+      const double t = ((double)full * two + (rest > PLAN_SMS ? two : rest > 0 ? one : 0.0)) * per + (bm == 64 ? 2.0 : 4.0) + (q > 1 ? 1.0 : 0.0);
+      if (t < least) { least = t; best = FmaPlan{bm, q, per}; }
+    }
+  }
+  return best;
+}
+typedef void (*FmaFn)(const fp32::Args);
+template <int BM> FmaFn fma_fn(int act) {
+  return act == ABS_ACT_RELU ? (FmaFn)fp32::fma_kernel<BM, BM, ABS_ACT_RELU> : act == ABS_ACT_GELU ? (FmaFn)fp32::fma_kernel<BM, BM, ABS_ACT_GELU>
+         : act == ABS_ACT_SILU ? (FmaFn)fp32::fma_kernel<BM, BM, ABS_ACT_SILU> : (FmaFn)fp32::fma_kernel<BM, BM, ABS_ACT_NONE>;
+}
+int fma_product(fp32::Args p, long long I, int J, int K, int act, int device, cudaStream_t s) {
+  static std::atomic<uint64_t> ready;
+  cudaError_t e = cudaSuccess;
+  if (!(ready.load(std::memory_order_acquire) >> device & 1)) {
+    for (int i = ABS_ACT_NONE; i <= ABS_ACT_SILU && e == cudaSuccess; ++i) {
+      e = allow_smem(fma_fn<64>(i), fp32::Cfg<64, 64>::SMEM);
+      if (e == cudaSuccess) e = allow_smem(fma_fn<128>(i), fp32::Cfg<128, 128>::SMEM);
+    }
+    if (e != cudaSuccess) return fail(ABS_ECUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
+    ready.fetch_or(1ull << device, std::memory_order_release);
+  }
+  for (long long pitch : {p.a_i, p.a_k, p.b_k, p.b_j})
+    if (pitch > (1ll << 24)) return fail(ABS_EUNSUPPORTED, "fp32: row pitch %lld above 2^24", pitch);
+  const FmaPlan pl = plan_fma(I, J, K);
+  p.I = (int)I; p.J = J; p.K = K;
+  p.n_kb = (K + fp32::BK - 1) / fp32::BK;
+  p.n_jt = (J + pl.bm - 1) / pl.bm;
+  p.Q = pl.Q; p.kb_per = pl.kb_per;
+  p.by_Q = Divisor((uint32_t)pl.Q);
+  p.by_njt = Divisor((uint32_t)p.n_jt);
+  const long long ctas = (I + pl.bm - 1) / pl.bm * p.n_jt * pl.Q;
+  if (ctas > 0x7fffffff) return fail(ABS_EUNSUPPORTED, "%lld tiles in one product", ctas);
+  e = pl.bm == 64 ? launch(fma_fn<64>(act), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<64, 64>::SMEM, pl.Q, s, p)
+                  : launch(fma_fn<128>(act), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<128, 128>::SMEM, pl.Q, s, p);
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }
 
@@ -445,15 +441,19 @@ extern "C" int abs_linear(const void* x, long long ldx, const void* w, long long
   if (overlap(sp, sx) || overlap(sp, sw) || overlap(sp, sb) || overlap(sp, sr) || overlap(sp, sy)) return fail(ABS_EINVAL, "pre overlaps another matrix");
   if (overlap(sy, sr) && !(y == residual && ldy == ldr)) return fail(ABS_EINVAL, "y overlaps residual without being the same matrix");
   cudaStream_t s = (cudaStream_t)stream;
+  int device, sms;
+  if ((rc = current_device(&device, &sms)) != ABS_OK) return rc;
   if (dtype == ABS_FP32) {
-    const ProdArgs p = {x, w, ldx, 1, ldw, 1, rows, n_out, n_in, bias, residual, y, pre, ldr, ldy, ldp};
-    return run_product(p, act, s);
+    fp32::Args p = {};
+    p.a = (const float*)x; p.a_i = ldx; p.a_k = 1;
+    p.b = (const float*)w; p.b_k = ldw; p.b_j = 1;
+    p.bias = (const float*)bias; p.res = (const float*)residual; p.out = (float*)y; p.pre = (float*)pre;
+    p.ldr = ldr; p.ldo = ldy; p.ldp = ldp;
+    return fma_product(p, rows, n_out, n_in, act, device, s);
   }
   const bool pack_x = !tma_able(x, rows, ldx), pack_w = !tma_able(w, n_in, ldw);
   const FwdPlan f = fwd_plan(rows, n_in, n_out, dtype, pack_x, pack_w);
   if ((rc = check_scratch(scratch, scratch_bytes, f.total)) != ABS_OK) return rc;
-  int device, sms;
-  if ((rc = current_device(&device, &sms)) != ABS_OK) return rc;
   char* sc = (char*)scratch;
   Operand a = {x, rows, n_in, tma_pitch(rows, n_in, ldx)}, b = {w, n_in, n_out, tma_pitch(n_in, n_out, ldw)};
   if (pack_x) {
@@ -507,23 +507,31 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
   char* sc = (char*)scratch;
   const void* dz = need_dz ? sc + g.dz : dy;
   const long long lddz = need_dz ? g.ld_dz : lddy;
-  float* part = db ? (float*)(sc + g.sums) : nullptr;
+  const bool with_dw = !bf16 && dw && db;              // the column sums come with the product
+  float* part = db && !with_dw ? (float*)(sc + g.sums) : nullptr;
   cudaError_t e = cudaSuccess;
-  if (need_dz || db)
+  if (need_dz || part)
     e = launch(dtype == ABS_FP32 ? slope_fn<float>(act) : slope_fn<__nv_bfloat16>(act), dim3((unsigned)((n_out + 31) / 32), (unsigned)g.chunks), 256, 0, 1, s,
                dy, lddy, pre, ldp, need_dz ? (void*)(sc + g.dz) : (void*)nullptr, lddz, part, rows, n_out, g.chunk);
-  if (db && e == cudaSuccess)
+  if (part && e == cudaSuccess)
     e = launch(dtype == ABS_FP32 ? column_kernel<float> : column_kernel<__nv_bfloat16>, dim3((unsigned)((n_out + 255) / 256)), 256, 0, 1, s,
                (const float*)part, g.chunks, n_out, db);
   if (e != cudaSuccess) return fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
   if (!bf16) {
     if (dx) {
-      const ProdArgs p = {dz, w, lddz, 1, 1, ldw, rows, n_in, n_out, nullptr, nullptr, dx, nullptr, 0, lddx, 0};
-      if ((rc = run_product(p, ABS_ACT_NONE, s)) != ABS_OK) return rc;
+      fp32::Args p = {};
+      p.a = (const float*)dz; p.a_i = lddz; p.a_k = 1;
+      p.b = (const float*)w; p.b_k = 1; p.b_j = ldw;
+      p.out = (float*)dx; p.ldo = lddx;
+      if ((rc = fma_product(p, rows, n_in, n_out, ABS_ACT_NONE, device, s)) != ABS_OK) return rc;
     }
     if (dw) {
-      const ProdArgs p = {x, dz, 1, ldx, lddz, 1, n_in, n_out, rows, nullptr, nullptr, dw, nullptr, 0, lddw, 0};
-      if ((rc = run_product(p, ABS_ACT_NONE, s)) != ABS_OK) return rc;
+      fp32::Args p = {};
+      p.a = (const float*)x; p.a_i = 1; p.a_k = ldx;
+      p.b = (const float*)dz; p.b_k = lddz; p.b_j = 1;
+      p.out = (float*)dw; p.ldo = lddw;
+      p.colsum = with_dw ? (float*)db : nullptr;
+      if ((rc = fma_product(p, n_in, n_out, (int)rows, ABS_ACT_NONE, device, s)) != ABS_OK) return rc;
     }
     return ABS_OK;
   }

@@ -1,0 +1,250 @@
+// The products of the affine layer in fp32, on FP32 FMAs (no rounding of operands), two per instruction.
+//
+// C[i][j] = sum_k A(i, k) B(k, j); either operand has its sum index or its other index contiguous.  A CTA of 256 threads takes a
+// BM x BN tile; blocks of 32 k are copied a few ahead by 4-byte asynchronous copies, which take any pitch and alignment, put both
+// operands k-major into shared memory and fill what lies outside with zeros.  A thread holds 8 x 8 sums as pairs of neighbouring j: a
+// k costs four 16-byte shared loads and eight doublings of an operand of A per 32 packed FMAs.  (Products alone, without copies, by a
+// loop over shared memory: 61 TFLOP/s in this form, 59 with single FMAs, 50 to 57 with pairs of even and odd k, which need no doubling.)
+// 64 x 64 tiles have four groups of 64 threads that take eight k of a block each (KG = 4), added at
+// the end; and a cluster of Q CTAs can share a tile's sum: each leaves its part in shared memory, takes 1 / Q of the tile's rows,
+// adds the parts in the order of the ranks and applies the epilogue.
+#pragma once
+#include "layerops.cuh"
+
+namespace absb {
+namespace fp32 {
+
+constexpr int NT = 256, BK = 32, STAGES = 3;
+
+struct Args {
+  const float* a; const float* b;
+  long long a_i, a_k, b_k, b_j;          // element pitches; one of each pair is 1
+  int I, J, K;
+  int n_jt, Q, kb_per, n_kb;             // column tiles; CTAs per tile, blocks of 32 k of each
+  const float* bias; const float* res; float* out; float* pre;
+  long long ldr, ldo, ldp;
+  float* colsum;                         // sums of B's columns (null: none), by the CTAs of the first row tile
+  layer::Divisor by_Q, by_njt;
+};
+
+template <int BM, int BN> struct Cfg {
+  static constexpr int LDA = BM + 4, LDB = BN + 4;       // (4 modulo 32; with the swizzle no bank is hit twice, or twice at most)
+  static constexpr int KG = NT / ((BM / 8) * (BN / 8));
+  static constexpr int STAGE = BK * (LDA + LDB);
+  static constexpr size_t SMEM = (size_t)STAGES * STAGE * 4;
+};
+
+__device__ __forceinline__ float ld_peer(const float* p, int rank) {
+  uint32_t a = (uint32_t)__cvta_generic_to_shared(p), r;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(r) : "memory");
+  return v;
+}
+
+// Shared memory holds element (k, x) of an operand at [k][x ^ swizzle(k)]: where the sum index is contiguous in memory, a warp copies 32 k
+// of one x (whole lines), and would hit the same eight banks four times over.  Neighbouring pairs of B's columns stay pairs.
+__host__ __device__ constexpr int swizzle_a(int k) { return k >> 3; }
+__host__ __device__ constexpr int swizzle_b(int k) { return (k >> 4) << 1; }
+
+// This thread's part of one operand's copies: element n of a block goes from src + n * hop to its place in the tile.
+template <int W, bool B> struct Mover {
+  static constexpr int N = BK * W / NT, LD = W + 4;
+  static constexpr uint32_t ALL = N == 32 ? 0xffffffffu : (1u << N) - 1u;
+  const float* src;
+  long long advance;
+  int hop;                               // (a pitch that does not fit is refused by the host)
+  int k, x0;                             // k of element 0 inside a block, index along the tile of element 0
+  uint32_t rows;                         // k contiguous: which elements lie inside the matrix; else all or none
+  bool kmajor;
+  // X: elements of the matrix from the tile's start on
+  __device__ __forceinline__ Mover(const float* base, long long px, long long pk, long long x_tile, int X) {
+    kmajor = pk == 1;
+    if (kmajor) {                        // element n: x0 + 8 n
+      k = threadIdx.x & 31;
+      x0 = threadIdx.x >> 5;
+      hop = 8 * (int)px;
+      const int n = x0 < X ? (X - x0 + 7) / 8 : 0;
+      rows = n >= N ? ALL : (1u << n) - 1u;
+    } else {                             // element n: k + (NT / W) n
+      x0 = (int)threadIdx.x % W;
+      k = (int)threadIdx.x / W;
+      hop = (NT / W) * (int)pk;
+      rows = x0 < X ? ALL : 0u;
+    }
+    src = base + (x_tile + x0) * px + (long long)k * pk;
+    advance = BK * pk;
+  }
+  __device__ __forceinline__ void copy(float* tile, const float* any, int kb, int K) const {
+    const float* s = src + (long long)kb * advance;
+    const int left = K - kb * BK - k;    // (elements of the sum from this thread's first one on)
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(tile);
+    if (kmajor) {
+      const uint32_t d0 = d + 4u * (uint32_t)(k * LD + (x0 ^ (B ? swizzle_b(k) : swizzle_a(k))));
+      put(s, any, left > 0 ? rows : 0u, [&](int n) { return d0 + 32u * (uint32_t)n; });
+    } else {
+      uint32_t in = rows;
+      if (left < BK) {
+        const int n = left > 0 ? (left + NT / W - 1) / (NT / W) : 0;
+        in = n >= N ? in : in & ((1u << n) - 1u);
+      }
+      const uint32_t d0 = d + 4u * (uint32_t)(k * LD);
+      put(s, any, in, [&](int n) {       // (k < NT / W <= 4 does not reach the swizzle's bits)
+        const int up = (NT / W) * n;
+        return d0 + 4u * (uint32_t)(up * LD + (x0 ^ (B ? swizzle_b(up) : swizzle_a(up))));
+      });
+    }
+  }
+  template <typename F> __device__ __forceinline__ void put(const float* s, const float* any, uint32_t in, F at) const {
+    if (in == ALL) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(at(n)), "l"(s + (long long)hop * n) : "memory");
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;"
+                     ::"r"(at(n)), "l"(in >> n & 1u ? s + (long long)hop * n : any), "r"(in >> n & 1u ? 4 : 0) : "memory");
+    }
+  }
+};
+
+template <int BM, int BN, int ACT>
+__global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Args p) {
+  using C = Cfg<BM, BN>;
+  constexpr int KG = C::KG, KPG = BK / KG, TX = BN / 8;
+  extern __shared__ __align__(16) float sm[];
+  const uint32_t tile = p.by_Q.div(blockIdx.x);
+  const int rank = (int)(blockIdx.x - tile * p.by_Q.d);
+  const uint32_t it = p.by_njt.div(tile);
+  const long long i0 = (long long)it * BM;
+  const int j0 = (int)(tile - it * p.by_njt.d) * BN;
+  const int kb0 = rank * p.kb_per, nkb = min(p.kb_per, p.n_kb - kb0);
+  grid_dependency_sync();
+
+  const int X = (int)min((long long)BM, p.I - i0), Y = min(BN, p.J - j0);
+  const Mover<BM, false> ma(p.a, p.a_i, p.a_k, i0, X);
+  const Mover<BN, true> mb(p.b, p.b_j, p.b_k, j0, Y);
+  auto fetch = [&](int kb) {
+    if (kb < nkb) {
+      float* st = sm + (kb % STAGES) * C::STAGE;
+      ma.copy(st, p.a, kb0 + kb, p.K);
+      mb.copy(st + BK * C::LDA, p.b, kb0 + kb, p.K);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  for (int s = 0; s < STAGES - 1; ++s) fetch(s);
+
+  const int g = (int)threadIdx.x / (NT / KG), t = (int)threadIdx.x % (NT / KG);
+  const int tx = t % TX, ty = t / TX;
+  layer::Lanes<2> acc[8][4];
+#pragma unroll
+  for (int u = 0; u < 8; ++u)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) acc[u][v].fill(0.f);
+  float cs = 0.f;
+  const bool sums = p.colsum != nullptr && it == 0 && (int)threadIdx.x < BN;
+  for (int kb = 0; kb < nkb; ++kb) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+    __syncthreads();                     // the block is there, and everybody has left the one that is overwritten next
+    fetch(kb + STAGES - 1);
+    const float* sa = sm + (kb % STAGES) * C::STAGE + g * KPG * C::LDA + 4 * ty;
+    const float* sb = sm + (kb % STAGES) * C::STAGE + BK * C::LDA + g * KPG * C::LDB + 4 * tx;
+    // eight k have one swizzle: with one group of threads it is known here, with four it is the group's and goes into row_of, col_of
+#pragma unroll
+    for (int o = 0; o < KPG / 8; ++o) {
+      const int xa = KG == 1 ? swizzle_a(8 * o) : 0, xb = KG == 1 ? swizzle_b(8 * o) >> 1 : 0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k, sa += C::LDA, sb += C::LDB) {
+        const float4 a0 = *reinterpret_cast<const float4*>(sa), a1 = *reinterpret_cast<const float4*>(sa + BM / 2);
+        layer::Lanes<4> b0, b1;
+        b0.load(sb);
+        b1.load(sb + BN / 2);
+        const float av[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
+        layer::Lanes<2> bv[4];
+        bv[0].p[0] = b0.p[0]; bv[1].p[0] = b0.p[1]; bv[2].p[0] = b1.p[0]; bv[3].p[0] = b1.p[1];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          layer::Lanes<2> aa;
+          aa.fill(av[(u & 4) | ((u & 3) ^ xa)]);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) acc[u][v] = layer::fma(aa, bv[(v & 2) | ((v & 1) ^ xb)], acc[u][v]);
+        }
+      }
+    }
+    if (sums) {
+      const float* col = sm + (kb % STAGES) * C::STAGE + BK * C::LDA;
+#pragma unroll 8
+      for (int k = 0; k < BK; ++k) cs += col[k * C::LDB + ((int)threadIdx.x ^ swizzle_b(k))];
+    }
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();
+
+  // groups of threads, then the CTAs of the cluster; the tile is left in sm[BM][BN]
+  float* tile_sm = sm;
+  float* cs_sm = sm + BM * BN;           // [BN]  (BM x BN + BN floats fit into the stages)
+  const int ga = KG == 1 ? 0 : swizzle_a(g * KPG), gb = KG == 1 ? 0 : swizzle_b(g * KPG) >> 1;
+  auto row_of = [&](int u) { return (u < 4 ? 0 : BM / 2) + ty * 4 + ((u & 3) ^ ga); };
+  auto col_of = [&](int v) { return (v < 2 ? 0 : BN / 2) + tx * 4 + 2 * ((v & 1) ^ gb); };
+#pragma unroll 1
+  for (int h = KG - 1; h >= 0; --h) {
+    if (g == h) {
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          unsigned long long* d = reinterpret_cast<unsigned long long*>(tile_sm + row_of(u) * BN + col_of(v));
+          if (h < KG - 1) {
+            layer::Lanes<2> o;
+            o.p[0] = *d;
+            acc[u][v] = layer::add(acc[u][v], o);
+          }
+          *d = acc[u][v].p[0];
+        }
+    }
+    __syncthreads();
+  }
+  if (sums) cs_sm[threadIdx.x] = cs;
+  if (p.Q > 1) {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  } else {
+    __syncthreads();
+  }
+  const int share = (BM + p.Q - 1) / p.Q, r0 = rank * share, r1 = min(min(BM, r0 + share), X);
+  for (int e = (int)threadIdx.x; e < (r1 - r0) * BN; e += NT) {
+    const int r = r0 + e / BN, c = e % BN;
+    if (c >= Y) continue;
+    float z = 0.f;
+    if (p.Q > 1) {
+      float part[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) part[q] = q < p.Q ? ld_peer(tile_sm + r * BN + c, q) : 0.f;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) z += part[q];
+    } else {
+      z = tile_sm[r * BN + c];
+    }
+    const long long i = i0 + r;
+    const int j = j0 + c;
+    if (p.bias) z += p.bias[j];
+    if (p.pre) p.pre[i * p.ldp + j] = z;
+    float y = layer::act_value<ACT>(z);
+    if (p.res) y += p.res[i * p.ldr + j];
+    p.out[i * p.ldo + j] = y;
+  }
+  if (sums && rank == 0 && (int)threadIdx.x < Y) {
+    float z = cs;
+    for (int q = 1; q < p.Q; ++q) z += ld_peer(cs_sm + threadIdx.x, q);
+    p.colsum[j0 + threadIdx.x] = z;
+  }
+  if (p.Q > 1) {                         // nobody leaves while a peer reads its part
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+}
+
+}  // namespace fp32
+}  // namespace absb
