@@ -327,9 +327,9 @@ int abs_linear_grad(const void* dy, long long lddy, const void* x, long long ldx
                     long long rows, int n_in, int n_out, int act, int dtype, void* scratch, size_t scratch_bytes,
                     void* stream);
 
-/* Scratch of abs_linear (grad = 0) or abs_linear_grad (grad = 1).  aligned = 1 if every matrix of
- * the call starts on a 16-byte boundary and has a row pitch that is a multiple of 16 bytes; 0
- * covers every call. */
+/* Scratch of abs_linear (grad = 0) or abs_linear_grad (grad = 1).  aligned: the sum of 1 for x, 2 for w
+ * and 4 for dy, each if that matrix starts on a 16-byte boundary and has a row pitch that is a multiple
+ * of 16 bytes (or one row); 0 covers every call. */
 int abs_linear_scratch_bytes(long long rows, int n_in, int n_out, int act, int dtype, int grad, int aligned, size_t* out);
 
 /* Dropout with a mask that is never stored: y = (kept ? x * s : 0) + residual (NULL: none), on

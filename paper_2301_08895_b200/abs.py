@@ -6,6 +6,8 @@ stream.  There is no CPU fallback: if the library has not been built, or no
 CUDA device is present, the calls raise.
 """
 import ctypes as C
+import functools
+import math
 import os
 
 import numpy as np
@@ -346,101 +348,127 @@ def lsq_gradient_noalloc(X, y, w, idx, g_out, loss_out, stream=None):
                                           loss_out.data_ptr(), _raw_stream(torch, stream, X)))
 
 
-# ---- layer operations on torch CUDA tensors
+# ---- layer operations on torch CUDA tensors.  A call's tensors have one type and one device, which is made current for the call
+# where it is not; the checks and addresses are plain function calls because a small call's time is the host's.
 
-def _torch():
-    global _torch_mod, _STORED
-    if _torch_mod is None:
+_STORED = {}          # torch.float32 -> FP32, torch.bfloat16 -> BF16_FP32MASTER
+_torch = None
+
+
+def _begin(first, stream):
+    """(dtype code, device index, cudaStream_t) of a call on tensors like `first`."""
+    global _torch
+    if _torch is None:
         import torch
-        _torch_mod = torch
-        _STORED = {torch.float32: FP32, torch.bfloat16: BF16_FP32MASTER}
-    return _torch_mod
+        _STORED.update({torch.float32: FP32, torch.bfloat16: BF16_FP32MASTER})
+        _torch = torch
+    code = _STORED.get(first.dtype)
+    if code is None:
+        raise ValueError("expected float32 or bfloat16 tensors, got %s" % first.dtype)
+    device = first.get_device()
+    if stream is None:
+        return code, device, _raw_stream(_torch, None, first)
+    if stream.device_index != device:
+        raise ValueError("the stream belongs to device %d, the tensors are on %s" % (stream.device_index, first.device))
+    return code, device, stream.cuda_stream
 
 
-_torch_mod = None
-_STORED = {}
+def _refuse(name, t, shape, dtype, device):
+    if t.dtype is not dtype or t.get_device() != device:
+        raise ValueError("%s: expected %s on cuda:%d, got %s on %s" % (name, dtype, device, t.dtype, t.device))
+    raise ValueError("%s: expected shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
 
 
-class _Call:
-    """The tensors of one call: one type, one device, which is made current for the call; their addresses, and the stream."""
-
-    def __init__(self, first, stream):
-        torch = _torch()
-        self.dtype = first.dtype
-        self.code = _STORED.get(first.dtype, -1)
-        if self.code < 0:
-            raise ValueError("expected float32 or bfloat16 tensors, got %s" % first.dtype)
-        self.device = first.get_device()
-        if self.device < 0:
-            raise ValueError("expected a tensor on a CUDA device, got one on %s" % first.device)
-        if stream is None:
-            self.stream = _raw_stream(torch, None, first)
-        else:
-            if stream.device_index != self.device:
-                raise ValueError("the stream belongs to device %d, the tensors to device %d" % (stream.device_index, self.device))
-            self.stream = stream.cuda_stream
-        self.owner = stream
-
-    def tensor(self, name, t, shape, dtype=None):
-        """Address of a tensor of this call (0: None) whose last dimension is contiguous."""
-        if t is None:
-            return 0
-        if t.dtype is not (dtype or self.dtype) or t.get_device() != self.device:
-            raise ValueError("%s: expected %s on cuda:%d, got %s on %s" % (name, dtype or self.dtype, self.device, t.dtype, t.device))
-        if t.shape != shape:
-            raise ValueError("%s: expected shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-        if shape[-1] > 1 and t.stride(-1) != 1:
-            raise ValueError("%s: the last dimension must be contiguous" % name)
-        return t.data_ptr()
-
-    def matrix(self, name, t, rows, cols):
-        """(address, row pitch) of a matrix."""
-        ptr = self.tensor(name, t, (rows, cols))
-        return ptr, (t.stride(0) if ptr and rows > 1 else cols)
-
-    def maps(self, name, t, shape):
-        """(address, sample pitch, position pitch) of channels-last maps [samples, ..., channels]."""
-        ptr = self.tensor(name, t, shape)
-        if not ptr:
-            return 0, 0, 0
-        pitch, span = shape[-1], 1
-        for d in range(len(shape) - 2, 0, -1):       # positions: one common pitch
-            if shape[d] > 1:
-                if span == 1:
-                    pitch = t.stride(d)
-                elif t.stride(d) != pitch * span:
-                    raise ValueError("%s: the positions of a sample must have one common pitch" % name)
-                span *= shape[d]
-        return ptr, t.stride(0), pitch
-
-    def scratch(self, given, need):
-        """(address, bytes, tensor) of scratch: the caller's, or one allocated for the call on its stream."""
-        if given is not None:
-            if given.get_device() != self.device or not given.is_contiguous():
-                raise ValueError("scratch: expected a contiguous tensor on cuda:%d" % self.device)
-            return given.data_ptr(), given.numel() * given.element_size(), given
-        if not need:
-            return 0, 0, None
-        torch = _torch()
-        if self.owner is None:
-            t = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", self.device))
-        else:
-            with torch.cuda.stream(self.owner):
-                t = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", self.device))
-        return t.data_ptr(), need, t
-
-    def run(self, fn, *args):
-        torch = _torch()
-        if torch.cuda.current_device() == self.device:
-            _check(fn(*args))
-        else:
-            with torch.cuda.device(self.device):
-                _check(fn(*args))
+def _matrix(name, t, shape, dtype, device):
+    """(address, row pitch) of a matrix whose rows are contiguous; (0, columns) of None."""
+    if t is None:
+        return 0, shape[1]
+    if t.dtype is not dtype or t.get_device() != device or t.shape != shape:
+        _refuse(name, t, shape, dtype, device)
+    pitch, unit = t.stride()
+    if unit != 1 and shape[1] > 1:
+        raise ValueError("%s: the last dimension must be contiguous" % name)
+    return t.data_ptr(), pitch if shape[0] > 1 else shape[1]
 
 
-def linear_scratch_bytes(rows, n_in, n_out, act=ACT_NONE, dtype=BF16_FP32MASTER, grad=False, aligned=False):
-    """abs_linear_scratch_bytes: scratch of `linear` or `linear_grad`; aligned: every matrix starts on a 16-byte
-    boundary and has a row pitch that is a multiple of 16 bytes."""
+def _vector(name, t, n, dtype, device):
+    """Address of a contiguous vector, 0 of None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.get_device() != device or t.shape != (n,):
+        _refuse(name, t, (n,), dtype, device)
+    if n > 1 and t.stride(0) != 1:
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr()
+
+
+def _maps(name, t, shape, dtype, device):
+    """(address, sample pitch, position pitch) of channels-last maps [samples, ..., channels] whose positions have one pitch."""
+    if t is None:
+        return 0, 0, 0
+    if t.dtype is not dtype or t.get_device() != device or t.shape != shape:
+        _refuse(name, t, shape, dtype, device)
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
+        raise ValueError("%s: the last dimension must be contiguous" % name)
+    pitch, span = shape[-1], 1
+    for d in range(len(shape) - 2, 0, -1):
+        if shape[d] > 1:
+            if span == 1:
+                pitch = strides[d]
+            elif strides[d] != pitch * span:
+                raise ValueError("%s: the positions of a sample must have one common pitch" % name)
+            span *= shape[d]
+    return t.data_ptr(), strides[0], pitch
+
+
+def _stats(name, t, shape, device):
+    """Address of contiguous float32 statistics [samples, groups], 0 of None."""
+    if t is None:
+        return 0
+    if t.dtype is not _torch.float32 or t.get_device() != device or t.shape != shape:
+        _refuse(name, t, shape, _torch.float32, device)
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr()
+
+
+@functools.lru_cache(maxsize=None)
+def _device(index):
+    return _torch.device("cuda", index)
+
+
+def _scratch(given, need, device, stream):
+    """(address, bytes, tensor) of scratch: the caller's, or one allocated for the call, on its stream."""
+    if given is not None:
+        if given.get_device() != device or not given.is_contiguous():
+            raise ValueError("scratch: expected a contiguous tensor on cuda:%d" % device)
+        return given.data_ptr(), given.numel() * given.element_size(), given
+    if not need:
+        return 0, 0, None
+    where = _device(device)
+    if stream is None:
+        t = _torch.empty(need, dtype=_torch.uint8, device=where)
+    else:
+        with _torch.cuda.stream(stream):
+            t = _torch.empty(need, dtype=_torch.uint8, device=where)
+    return t.data_ptr(), need, t
+
+
+def _run(device, fn, *args):
+    if _torch.cuda.current_device() == device:
+        rc = fn(*args)
+    else:
+        with _torch.cuda.device(device):
+            rc = fn(*args)
+    if rc != OK:
+        raise AbsError(rc, last_error())
+
+
+@functools.lru_cache(maxsize=4096)
+def linear_scratch_bytes(rows, n_in, n_out, act=ACT_NONE, dtype=BF16_FP32MASTER, grad=False, aligned=0):
+    """abs_linear_scratch_bytes: scratch of `linear` or `linear_grad`; aligned: the sum of 1 for x, 2 for w and 4 for dy,
+    each if it starts on a 16-byte boundary and has a row pitch that is a multiple of 16 bytes; 0 covers every call."""
     out = C.c_size_t(0)
     _check(lib().abs_linear_scratch_bytes(rows, n_in, n_out, act, dtype, int(grad), int(aligned), C.byref(out)))
     return out.value
@@ -453,16 +481,17 @@ def linear(x, w, bias, residual, y, act=ACT_NONE, pre=None, scratch=None, stream
     one allocated on the call's stream."""
     rows, n_in = x.shape
     n_out = w.shape[1]
-    c = _Call(x, stream)
-    xp, ldx = c.matrix("x", x, rows, n_in)
-    wp, ldw = c.matrix("w", w, n_in, n_out)
-    bp = c.tensor("bias", bias, (n_out,))
-    rp, ldr = c.matrix("residual", residual, rows, n_out)
-    yp, ldy = c.matrix("y", y, rows, n_out)
-    pp, ldp = c.matrix("pre", pre, rows, n_out)
-    aligned = ((xp | wp | rp | yp | pp) | ((ldx | ldw | ldr | ldy | ldp) * x.element_size())) & 15 == 0
-    sp, sz, keep = c.scratch(scratch, linear_scratch_bytes(rows, n_in, n_out, act, c.code, False, aligned))
-    c.run(lib().abs_linear, xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, pp, ldp, rows, n_in, n_out, act, c.code, sp, sz, c.stream)
+    code, dev, s = _begin(x, stream)
+    dt, out = x.dtype, (rows, n_out)
+    xp, ldx = _matrix("x", x, (rows, n_in), dt, dev)
+    wp, ldw = _matrix("w", w, (n_in, n_out), dt, dev)
+    bp = _vector("bias", bias, n_out, dt, dev)
+    rp, ldr = _matrix("residual", residual, out, dt, dev)
+    yp, ldy = _matrix("y", y, out, dt, dev)
+    pp, ldp = _matrix("pre", pre, out, dt, dev)
+    aligned = 0 if code == FP32 else ((xp | (ldx << 1 if rows > 1 else 0)) & 15 == 0) + 2 * ((wp | (ldw << 1 if n_in > 1 else 0)) & 15 == 0)
+    sp, sz, keep = _scratch(scratch, linear_scratch_bytes(rows, n_in, n_out, act, code, False, aligned), dev, stream)
+    _run(dev, lib().abs_linear, xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, pp, ldp, rows, n_in, n_out, act, code, sp, sz, s)
 
 
 def linear_grad(dy, x, w, pre, dx, dw, db, act=ACT_NONE, scratch=None, stream=None):
@@ -470,33 +499,38 @@ def linear_grad(dy, x, w, pre, dx, dw, db, act=ACT_NONE, scratch=None, stream=No
     (None: not wanted); pre as `linear` left it (None with ACT_NONE).  The residual's gradient is dy itself."""
     rows, n_in = x.shape
     n_out = w.shape[1]
-    c = _Call(x, stream)
-    gp, ldg = c.matrix("dy", dy, rows, n_out)
-    xp, ldx = c.matrix("x", x, rows, n_in)
-    wp, ldw = c.matrix("w", w, n_in, n_out)
-    pp, ldp = c.matrix("pre", pre, rows, n_out)
-    dxp, lddx = c.matrix("dx", dx, rows, n_in)
-    dwp, lddw = c.matrix("dw", dw, n_in, n_out)
-    dbp = c.tensor("db", db, (n_out,))
-    aligned = ((gp | xp | wp | pp | dxp | dwp) | ((ldg | ldx | ldw | ldp | lddx | lddw) * x.element_size())) & 15 == 0
-    sp, sz, keep = c.scratch(scratch, linear_scratch_bytes(rows, n_in, n_out, act, c.code, True, aligned))
-    c.run(lib().abs_linear_grad, gp, ldg, xp, ldx, wp, ldw, pp, ldp, dxp, lddx, dwp, lddw, dbp, rows, n_in, n_out, act, c.code,
-          sp, sz, c.stream)
+    code, dev, s = _begin(x, stream)
+    dt, out, wide, square = x.dtype, (rows, n_out), (rows, n_in), (n_in, n_out)
+    gp, ldg = _matrix("dy", dy, out, dt, dev)
+    xp, ldx = _matrix("x", x, wide, dt, dev)
+    wp, ldw = _matrix("w", w, square, dt, dev)
+    pp, ldp = _matrix("pre", pre, out, dt, dev)
+    dxp, lddx = _matrix("dx", dx, wide, dt, dev)
+    dwp, lddw = _matrix("dw", dw, square, dt, dev)
+    dbp = _vector("db", db, n_out, dt, dev)
+    many = rows > 1
+    aligned = 0 if code == FP32 else ((xp | (ldx << 1 if many else 0)) & 15 == 0) + 2 * ((wp | (ldw << 1 if n_in > 1 else 0)) & 15 == 0) + \
+        4 * ((gp | (ldg << 1 if many else 0)) & 15 == 0)
+    sp, sz, keep = _scratch(scratch, linear_scratch_bytes(rows, n_in, n_out, act, code, True, aligned), dev, stream)
+    _run(dev, lib().abs_linear_grad, gp, ldg, xp, ldx, wp, ldw, pp, ldp, dxp, lddx, dwp, lddw, dbp, rows, n_in, n_out, act, code,
+         sp, sz, s)
 
 
 def dropout(x, residual, y, p, seed, call, stream=None):
     """abs_dropout on matrices [rows, cols]: y = (kept ? x / (1 - p) : 0) + residual (or None); the mask is a function of
     element, `seed` and `call` (the number of the application: below 2^32).  The gradient is the same call on dy."""
-    rows, cols = x.shape
-    c = _Call(x, stream)
-    xp, ldx = c.matrix("x", x, rows, cols)
-    rp, ldr = c.matrix("residual", residual, rows, cols)
-    yp, ldy = c.matrix("y", y, rows, cols)
+    shape = rows, cols = x.shape
+    code, dev, s = _begin(x, stream)
+    dt = x.dtype
+    xp, ldx = _matrix("x", x, shape, dt, dev)
+    rp, ldr = _matrix("residual", residual, shape, dt, dev)
+    yp, ldy = _matrix("y", y, shape, dt, dev)
     if not 0 <= call < 1 << 32 or not 0 <= seed < 1 << 64:
         raise ValueError("call must be in [0, 2^32) and seed in [0, 2^64)")
-    c.run(lib().abs_dropout, xp, ldx, rp, ldr, yp, ldy, rows, cols, p, seed, call, c.code, c.stream)
+    _run(dev, lib().abs_dropout, xp, ldx, rp, ldr, yp, ldy, rows, cols, p, seed, call, code, s)
 
 
+@functools.lru_cache(maxsize=4096)
 def group_norm_scratch_bytes(samples, positions, channels, groups, dtype=BF16_FP32MASTER, grad=False):
     """abs_group_norm_scratch_bytes: scratch of `group_norm` or `group_norm_grad`."""
     out = C.c_size_t(0)
@@ -504,55 +538,43 @@ def group_norm_scratch_bytes(samples, positions, channels, groups, dtype=BF16_FP
     return out.value
 
 
-def op_status(stream=None):
-    """abs_op_status on the current device: waits for `stream` (default: the current one) and raises AbsError(ETIMEOUT) if a
-    bounded wait of a layer operation ran out since the last call."""
-    s = stream if stream is not None else _torch().cuda.current_stream()
-    _check(lib().abs_op_status(s.cuda_stream))
-
-
-def _positions(shape):
-    n = 1
-    for d in shape[1:-1]:
-        n *= d
-    return n
-
-
 def group_norm(x, groups, w, b, y, mean, rstd, eps=1e-5, act=ACT_NONE, scratch=None, stream=None):
     """abs_group_norm: y = act(group_norm(x) w + b) on channels-last maps [samples, ..., channels]; w, b [channels] or
     None; mean, rstd float32 [samples, groups] for `group_norm_grad`, or both None."""
-    c = _Call(x, stream)
-    shape = x.shape
-    n, pos, ch = shape[0], _positions(shape), shape[-1]
-    xp, xs, xq = c.maps("x", x, shape)
-    yp, ys, yq = c.maps("y", y, shape)
-    wp, bp = c.tensor("w", w, (ch,)), c.tensor("b", b, (ch,))
-    f32 = _torch().float32
-    mp, rp = c.tensor("mean", mean, (n, groups), f32), c.tensor("rstd", rstd, (n, groups), f32)
-    if n > 1 and ((mp and mean.stride(0) != groups) or (rp and rstd.stride(0) != groups)):
-        raise ValueError("mean and rstd must be contiguous")
-    sp, sz, keep = c.scratch(scratch, group_norm_scratch_bytes(n, pos, ch, groups, c.code, False))
-    c.run(lib().abs_group_norm, xp, xs, xq, wp, bp, yp, ys, yq, mp, rp, n, pos, ch, groups, eps, act, c.code, sp, sz, c.stream)
+    code, dev, s = _begin(x, stream)
+    shape, dt = x.shape, x.dtype
+    n, pos, ch = shape[0], math.prod(shape[1:-1]), shape[-1]
+    xp, xs, xq = _maps("x", x, shape, dt, dev)
+    yp, ys, yq = _maps("y", y, shape, dt, dev)
+    wp, bp = _vector("w", w, ch, dt, dev), _vector("b", b, ch, dt, dev)
+    mp, rp = _stats("mean", mean, (n, groups), dev), _stats("rstd", rstd, (n, groups), dev)
+    sp, sz, keep = _scratch(scratch, group_norm_scratch_bytes(n, pos, ch, groups, code, False), dev, stream)
+    _run(dev, lib().abs_group_norm, xp, xs, xq, wp, bp, yp, ys, yq, mp, rp, n, pos, ch, groups, eps, act, code, sp, sz, s)
 
 
 def group_norm_grad(dy, x, groups, w, b, mean, rstd, dx, dw, db, act=ACT_NONE, scratch=None, stream=None):
     """abs_group_norm_grad: dx (or None), dw and db [channels] (or None) of `group_norm` from dy and the mean and rstd
     that the forward pass stored."""
-    c = _Call(x, stream)
-    shape = x.shape
-    n, pos, ch = shape[0], _positions(shape), shape[-1]
-    gp, gs, gq = c.maps("dy", dy, shape)
-    xp, xs, xq = c.maps("x", x, shape)
-    dxp, dxs, dxq = c.maps("dx", dx, shape)
-    wp, bp = c.tensor("w", w, (ch,)), c.tensor("b", b, (ch,))
-    dwp, dbp = c.tensor("dw", dw, (ch,)), c.tensor("db", db, (ch,))
-    f32 = _torch().float32
-    mp, rp = c.tensor("mean", mean, (n, groups), f32), c.tensor("rstd", rstd, (n, groups), f32)
-    if n > 1 and ((mp and mean.stride(0) != groups) or (rp and rstd.stride(0) != groups)):
-        raise ValueError("mean and rstd must be contiguous")
-    sp, sz, keep = c.scratch(scratch, group_norm_scratch_bytes(n, pos, ch, groups, c.code, True))
-    c.run(lib().abs_group_norm_grad, gp, gs, gq, xp, xs, xq, wp, bp, mp, rp, dxp, dxs, dxq, dwp, dbp, n, pos, ch, groups, act,
-          c.code, sp, sz, c.stream)
+    code, dev, s = _begin(x, stream)
+    shape, dt = x.shape, x.dtype
+    n, pos, ch = shape[0], math.prod(shape[1:-1]), shape[-1]
+    gp, gs, gq = _maps("dy", dy, shape, dt, dev)
+    xp, xs, xq = _maps("x", x, shape, dt, dev)
+    dxp, dxs, dxq = _maps("dx", dx, shape, dt, dev)
+    wp, bp = _vector("w", w, ch, dt, dev), _vector("b", b, ch, dt, dev)
+    dwp, dbp = _vector("dw", dw, ch, dt, dev), _vector("db", db, ch, dt, dev)
+    mp, rp = _stats("mean", mean, (n, groups), dev), _stats("rstd", rstd, (n, groups), dev)
+    sp, sz, keep = _scratch(scratch, group_norm_scratch_bytes(n, pos, ch, groups, code, True), dev, stream)
+    _run(dev, lib().abs_group_norm_grad, gp, gs, gq, xp, xs, xq, wp, bp, mp, rp, dxp, dxs, dxq, dwp, dbp, n, pos, ch, groups, act,
+         code, sp, sz, s)
+
+
+def op_status(stream=None):
+    """abs_op_status on the current device: waits for `stream` (default: the current one) and raises AbsError(ETIMEOUT) if a
+    bounded wait of a layer operation ran out since the last call."""
+    import torch
+    s = stream if stream is not None else torch.cuda.current_stream()
+    _check(lib().abs_op_status(s.cuda_stream))
 
 
 def trace_rows(tr):

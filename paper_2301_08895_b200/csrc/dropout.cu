@@ -7,7 +7,7 @@ using namespace absb::layer;
 
 namespace {
 
-constexpr int DROP_NT = 256, DROP_U = 4;     // threads; blocks of eight columns per thread, loaded before the first is used
+constexpr int DROP_NT = 256;                 // threads; a thread takes U blocks of eight columns, all loaded before the first is used
 
 struct DropArgs {
   const void* x; const void* r; void* y;
@@ -50,18 +50,18 @@ __device__ __forceinline__ void load8(Eight<T>& e, const T* p, int n) {
   e.set(v);
 }
 
-template <typename T, bool VEC, bool RES>
+template <typename T, bool VEC, bool RES, int U>
 __global__ void __launch_bounds__(DROP_NT) dropout_kernel(DropArgs a) {
   grid_dependency_sync();
   const T* x = (const T*)a.x;
   const T* r = (const T*)a.r;
   T* y = (T*)a.y;
-  const uint32_t u0 = blockIdx.x * (uint32_t)(DROP_NT * DROP_U) + threadIdx.x;
-  Eight<T> ex[DROP_U], er[DROP_U];
-  uint32_t row[DROP_U], blk[DROP_U];
-  int n[DROP_U];
+  const uint32_t u0 = blockIdx.x * (uint32_t)(DROP_NT * U) + threadIdx.x;
+  Eight<T> ex[U], er[U];
+  uint32_t row[U], blk[U];
+  int n[U];
 #pragma unroll
-  for (int k = 0; k < DROP_U; ++k) {
+  for (int k = 0; k < U; ++k) {
     const uint32_t u = u0 + k * DROP_NT;
     const bool in = u < a.units;
     const uint32_t q = a.per_row.div(in ? u : 0u);
@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(DROP_NT) dropout_kernel(DropArgs a) {
     if (RES) load8<T, VEC>(er[k], r + (long long)row[k] * a.ldr + 8ll * blk[k], n[k]);
   }
 #pragma unroll
-  for (int k = 0; k < DROP_U; ++k) {
+  for (int k = 0; k < U; ++k) {
     if (n[k] == 0) break;
     uint32_t w[4];
     philox4x32_10(blk[k], row[k], 2u, a.call, a.key0, a.key1, w);
@@ -98,9 +98,9 @@ __global__ void __launch_bounds__(DROP_NT) dropout_kernel(DropArgs a) {
   }
 }
 
-template <typename T> void (*dropout_fn(bool vec, bool res))(DropArgs) {
-  if (vec) return res ? dropout_kernel<T, true, true> : dropout_kernel<T, true, false>;
-  return res ? dropout_kernel<T, false, true> : dropout_kernel<T, false, false>;
+template <typename T, int U> void (*dropout_fn(bool vec, bool res))(DropArgs) {
+  if (vec) return res ? dropout_kernel<T, true, true, U> : dropout_kernel<T, true, false, U>;
+  return res ? dropout_kernel<T, false, true, U> : dropout_kernel<T, false, false, U>;
 }
 
 }  // namespace
@@ -136,14 +136,17 @@ extern "C" int abs_dropout(const void* x, long long ldx, const void* residual, l
   a.key1 = (uint32_t)(seed >> 32);
   const bool vec = (((uintptr_t)x | (uintptr_t)y | (uintptr_t)residual | (uintptr_t)(ldx * (long long)esz) | (uintptr_t)(ldy * (long long)esz) |
                      (residual ? (uintptr_t)(ldr * (long long)esz) : 0)) & 15) == 0;
-  void (*kernel)(DropArgs) = dtype == ABS_FP32 ? dropout_fn<float>(vec, residual != nullptr) : dropout_fn<__nv_bfloat16>(vec, residual != nullptr);
+  // four blocks per thread, or one where that leaves SMs without work (128 x 256: 4.1 -> @ONE@ us)
+  const int U = rows * per_row > 2ll * PLAN_SMS * DROP_NT * 4 ? 4 : 1;
+  void (*kernel)(DropArgs) = dtype == ABS_FP32 ? (U == 4 ? dropout_fn<float, 4>(vec, residual != nullptr) : dropout_fn<float, 1>(vec, residual != nullptr))
+                                               : (U == 4 ? dropout_fn<__nv_bfloat16, 4>(vec, residual != nullptr) : dropout_fn<__nv_bfloat16, 1>(vec, residual != nullptr));
   // unit numbers are 32-bit: at most 2^30 blocks per launch
   const long long step = (1ll << 30) / per_row;
   for (long long r0 = 0; r0 < rows; r0 += step) {
     const long long nr = rows - r0 < step ? rows - r0 : step;
     a.row0 = (uint32_t)r0;
     a.units = (uint32_t)(nr * per_row);
-    const cudaError_t e = launch(kernel, dim3((a.units + DROP_NT * DROP_U - 1) / (DROP_NT * DROP_U)), DROP_NT, 0, 1, (cudaStream_t)stream, a);
+    const cudaError_t e = launch(kernel, dim3((a.units + DROP_NT * U - 1) / (DROP_NT * U)), DROP_NT, 0, 1, (cudaStream_t)stream, a);
     if (e != cudaSuccess) return fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
   }
   return ABS_OK;

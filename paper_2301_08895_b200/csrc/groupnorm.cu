@@ -98,11 +98,11 @@ template <int N> __device__ __forceinline__ void column_sums(const float* red, f
     }
   }
 }
-// f(g, sum of channels [lo, hi) of group g over all segments) for each group of the CTA: a thread to a group of few channels, else
+// f(g, sum of channels [lo, hi) of group g over all segments) for each group of the CTA: a thread to a group of few terms, else
 // a warp.  range(g, lo, hi) gives the channels.
 template <int N, typename Range, typename F>
 __device__ __forceinline__ void group_sums(const float* col, int segments, int cw, int groups, int D, Range range, F f) {
-  if (D <= 32) {
+  if (segments * D <= 16) {
     for (int g = threadIdx.x; g < groups; g += N) {
       int lo, hi;
       range(g, lo, hi);
@@ -118,8 +118,14 @@ __device__ __forceinline__ void group_sums(const float* col, int segments, int c
       int lo, hi;
       range(g, lo, hi);
       float t = 0.f;
-      for (int s = 0; s < segments; ++s)
-        for (int c = lo + lane; c < hi; c += 32) t += col[s * cw + c];
+      if (D <= 16) {                     // several segments at a time
+        const int k = 32 / D, s0 = lane / D, c = lo + lane - s0 * D;
+        if (s0 < k && c < hi)
+          for (int s = s0; s < segments; s += k) t += col[s * cw + c];
+      } else {
+        for (int s = 0; s < segments; ++s)
+          for (int c = lo + lane; c < hi; c += 32) t += col[s * cw + c];
+      }
       t = warp_sum(t);
       if (lane == 0) f(g, t);
     }

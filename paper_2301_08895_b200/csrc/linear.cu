@@ -6,6 +6,7 @@
 #include "layerops.cuh"
 #include "linear_tc.cuh"
 #include "linear_fma.cuh"
+#include "linear_small.cuh"
 
 using namespace absb;
 using namespace absb::layer;
@@ -45,39 +46,95 @@ namespace {
 
 constexpr int BK_TERMS = tc::BK;
 
-// dz = dy act'(pre), rounded to storage, and the column sums of the unrounded dz over each block of rows
-template <typename T, int ACT>
-__global__ void __launch_bounds__(256) slope_kernel(const void* dy, long long lddy, const void* pre, long long ldp, void* dz, long long lddz, float* part,
-                                                    long long rows, int n, int chunk) {
+// dz = dy act'(pre), rounded to storage, and the column sums of the unrounded dz over each chunk of rows: one pass at HBM's pace
+// (8192 x 4096 bf16 GELU: @SLOPE@).  A thread takes VE columns of every R-th row, eight rows' loads under way.
+struct SlopeArgs {
+  const void* dy; const void* pre; void* dz; float* part;
+  long long lddy, ldp, lddz, rows;
+  int n, chunk, lv, R;                   // vectors of columns per CTA, thread rows
+  Divisor by_lv;
+};
+template <typename T, int VE, int ACT>
+__global__ void __launch_bounds__(256) slope_kernel(const SlopeArgs a) {
+  __shared__ __align__(16) float red[256 * VE];
+  const int r = (int)a.by_lv.div(threadIdx.x), v = (int)threadIdx.x - r * a.lv;
+  const int c = (blockIdx.x * a.lv + v) * VE;
+  const bool active = r < a.R && c < a.n;
   grid_dependency_sync();
-  __shared__ float red[8][33];
-  const int lane = threadIdx.x & 31, r = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
-  const long long m0 = (long long)blockIdx.y * chunk, m1 = min(rows, m0 + chunk);
-  float s = 0.f;
-  if (j < n)
-    for (long long m = m0 + r; m < m1; m += 8) {
-      float g = ldf((const T*)dy, m * lddy + j);
-      if (ACT != ABS_ACT_NONE) g *= act_slope<ACT>(ldf((const T*)pre, m * ldp + j));
-      if (dz) stf((T*)dz, m * lddz + j, g);
-      s += g;
+  Lanes<VE> sum;
+  sum.fill(0.f);
+  if (active) {
+    const long long m0 = (long long)blockIdx.y * a.chunk, m1 = min(a.rows, m0 + a.chunk);
+    const T* dy = (const T*)a.dy + (m0 + r) * a.lddy + c;
+    const T* pre = (const T*)a.pre + (m0 + r) * a.ldp + c;
+    T* dz = (T*)a.dz + (m0 + r) * a.lddz + c;
+    const long long s0 = a.R * a.lddy, s1 = a.R * a.ldp, s2 = a.R * a.lddz;
+    constexpr int U = 4;
+    for (long long m = m0 + r; m < m1; m += U * a.R, dy += U * s0, pre += U * s1, dz += U * s2) {
+      Pack<T, VE> g[U], z[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (m + u * a.R < m1) {
+          g[u].load(dy + u * s0);
+          if (ACT != ABS_ACT_NONE) z[u].load(pre + u * s1);
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (m + u * a.R < m1) {
+          float f[VE];
+          Lanes<VE> l;
+          g[u].get(f);
+          l.set(f);
+          if (ACT != ABS_ACT_NONE) {
+            Lanes<VE> zl;
+            z[u].get(f);
+            zl.set(f);
+            l = mul(l, act_slopes<ACT>(zl));
+          }
+          sum = add(sum, l);
+          if (a.dz) {
+            l.get(f);
+            g[u].set(f);
+            g[u].store(dz + u * s2);
+          }
+        }
     }
-  red[r][lane] = s;
+  }
+  if (a.part == nullptr) return;
+  const int cb = a.lv * VE;
+  float f[VE];
+  sum.get(f);
+  if (active)
+#pragma unroll
+    for (int e = 0; e < VE; ++e) red[r * cb + v * VE + e] = f[e];
   __syncthreads();
-  if (r == 0 && j < n && part) {
+  for (int i = threadIdx.x; i < cb && blockIdx.x * cb + i < a.n; i += 256) {
     float t = 0.f;
-    for (int k = 0; k < 8; ++k) t += red[k][lane];
-    part[(size_t)blockIdx.y * n + j] = t;
+#pragma unroll 4
+    for (int k = 0; k < a.R; ++k) t += red[k * cb + i];
+    a.part[(size_t)blockIdx.y * a.n + blockIdx.x * cb + i] = t;
   }
 }
 
+// db = sum of the chunks' column sums: block = 32 columns x 8 rows of threads
 template <typename T>
 __global__ void __launch_bounds__(256) column_kernel(const float* part, int chunks, int n, void* db) {
+  __shared__ float red[8][33];
   grid_dependency_sync();
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= n) return;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
   float t = 0.f;
-  for (int c = 0; c < chunks; ++c) t += part[(size_t)c * n + j];
-  stf((T*)db, j, t);
+  if (j < n) {
+#pragma unroll 8
+    for (int c = w; c < chunks; c += 8) t += part[(size_t)c * n + j];
+  }
+  red[w][lane] = t;
+  __syncthreads();
+  if (w == 0 && j < n) {
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v += red[k][lane];
+    stf((T*)db, j, v);
+  }
 }
 
 // Partial results of a split sum: C = epilogue(sum over splits), in order.
@@ -131,10 +188,13 @@ __global__ void __launch_bounds__(256) pack_kernel(const __nv_bfloat16* src, lon
   }
 }
 
-typedef void (*SlopeFn)(const void*, long long, const void*, long long, void*, long long, float*, long long, int, int);
-template <typename T> SlopeFn slope_fn(int act) {
-  return act == ABS_ACT_RELU ? (SlopeFn)slope_kernel<T, ABS_ACT_RELU> : act == ABS_ACT_GELU ? (SlopeFn)slope_kernel<T, ABS_ACT_GELU>
-         : act == ABS_ACT_SILU ? (SlopeFn)slope_kernel<T, ABS_ACT_SILU> : (SlopeFn)slope_kernel<T, ABS_ACT_NONE>;
+typedef void (*SlopeFn)(const SlopeArgs);
+#define ACT_FN(type, name, act, ...)                                                                                       \
+  ((act) == ABS_ACT_RELU ? (type)name<__VA_ARGS__, ABS_ACT_RELU> : (act) == ABS_ACT_GELU ? (type)name<__VA_ARGS__, ABS_ACT_GELU> \
+   : (act) == ABS_ACT_SILU ? (type)name<__VA_ARGS__, ABS_ACT_SILU> : (type)name<__VA_ARGS__, ABS_ACT_NONE>)
+SlopeFn slope_fn(int dtype, bool vec, int act) {
+  if (dtype == ABS_FP32) return vec ? ACT_FN(SlopeFn, slope_kernel, act, float, 4) : ACT_FN(SlopeFn, slope_kernel, act, float, 1);
+  return vec ? ACT_FN(SlopeFn, slope_kernel, act, __nv_bfloat16, 8) : ACT_FN(SlopeFn, slope_kernel, act, __nv_bfloat16, 1);
 }
 typedef void (*FinishFn)(FinishArgs);
 FinishFn finish_fn(int act) {
@@ -149,12 +209,13 @@ size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 // How a product C[I][J] = sum over K terms is cut up.
 struct Plan { int bn, cg, splits, kb_per; size_t part_bytes; };
 
-// The cheapest of the four tiles and of the ways to split the sum, by a model in microseconds: a block of 64 terms of a tile,
-// the tiles a unit (CTA or CTA pair) takes in turn, a fixed part for filling the pipeline and the last tile's epilogue, and for
-// split sums the partial results' way through L2 and a second launch.
+// The cheapest of the five tiles and of the ways to split the sum, by a model in microseconds: a block of 64 terms of a tile (measured
+// at 8192 x 4096 x 4096: 178 us with 256 x 256 tiles of CTA pairs; the narrow tiles wait for operands, not for the tensor cores), the
+// tiles a unit (CTA or CTA pair) takes in turn, 4.1 us for launch, filling the pipeline and the last tile's epilogue, and for split sums the
+// partial results' way through L2 and a second launch.
 Plan plan_product(long long I, int J, long long K) {
-  struct Opt { int bn, cg; double kb, fixed; };
-  static const Opt opts[4] = {{256, 2, 0.34, 6.0}, {256, 1, 0.36, 5.5}, {128, 1, 0.22, 4.5}, {64, 1, 0.16, 4.0}};
+  struct Opt { int bn, cg; double kb; };
+  static const Opt opts[5] = {{256, 2, 0.40}, {256, 1, 0.45}, {128, 1, 0.29}, {128, 2, 0.29}, {64, 1, 0.28}};
   const long long n_kb = (K + BK_TERMS - 1) / BK_TERMS;
   const long long Jp = (J + 3) / 4 * 4;
   Plan best = {};
@@ -165,7 +226,7 @@ Plan plan_product(long long I, int J, long long K) {
     for (int s = 1; s <= 64 && s <= n_kb; ++s) {
       const long long per = (n_kb + s - 1) / s;
       if (s > 1 && ((s - 1) * per >= n_kb || (size_t)s * I * Jp * 4 > (256u << 20))) continue;
-      double t = (double)((tiles * s + units - 1) / units) * per * o.kb + o.fixed;
+      double t = (double)((tiles * s + units - 1) / units) * per * o.kb + 4.1;
       if (s > 1) t += 2.5 + (double)s * I * Jp * 8.0 / 6e6;
       if (t < best_t) {
         best_t = t;
@@ -282,7 +343,7 @@ int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, in
   mz = mo;
   if (p.pre_tma) ok = ok && matrix_map(&mz, r.pre, I, J, tma_pitch(I, J, r.ldp), 32);
   if (!ok) return fail(ABS_ECUDA, "cuTensorMapEncodeTiled failed");
-  cudaError_t e = pl.cg == 2 ? launch_dense<256, 2>(ma, mb, mo, mz, p, sms, device, s) : pl.bn == 256 ? launch_dense<256, 1>(ma, mb, mo, mz, p, sms, device, s)
+  cudaError_t e = pl.cg == 2 ? (pl.bn == 256 ? launch_dense<256, 2>(ma, mb, mo, mz, p, sms, device, s) : launch_dense<128, 2>(ma, mb, mo, mz, p, sms, device, s)) : pl.bn == 256 ? launch_dense<256, 1>(ma, mb, mo, mz, p, sms, device, s)
                   : pl.bn == 128 ? launch_dense<128, 1>(ma, mb, mo, mz, p, sms, device, s) : launch_dense<64, 1>(ma, mb, mo, mz, p, sms, device, s);
   if (e == cudaSuccess && pl.splits > 1) {
     FinishArgs f = {};
@@ -359,6 +420,58 @@ int fma_product(fp32::Args p, long long I, int J, int K, int act, int device, cu
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }
 
+// ------------------------------------------------------------------ few rows, few outputs
+
+// Rows up to which a pass over W on FP32 FMAs is faster than the tiled products: 784 -> 256 bf16 with 1, 2, 4 rows 3.5, 5.3, 8.9 us
+// against 6.8 us of the tensor-core product; 785 -> 501 fp32 with 8 rows 11.1 us, the FMA tiles as much.
+int few_rows_limit(int dtype) { return dtype == ABS_FP32 ? 8 : 2; }
+
+typedef void (*RowsFn)(const small::Args, int);
+template <typename T, int VE> RowsFn few_rows_fn(long long rows, int act) {
+  if constexpr (sizeof(T) == 4) {
+    if (rows > 4) return ACT_FN(RowsFn, small::few_rows_kernel, act, T, VE, 8);
+    if (rows > 2) return ACT_FN(RowsFn, small::few_rows_kernel, act, T, VE, 4);
+  }
+  return rows == 1 ? ACT_FN(RowsFn, small::few_rows_kernel, act, T, VE, 1) : ACT_FN(RowsFn, small::few_rows_kernel, act, T, VE, 2);
+}
+int few_rows(const small::Args& a, int dtype, cudaStream_t s) {
+  const size_t esz = dtype == ABS_FP32 ? 4 : 2;
+  const bool vec = (uintptr_t)a.w % 16 == 0 && (a.K == 1 || a.ldw * (long long)esz % 16 == 0) && (size_t)a.N * esz % 16 == 0;
+  const int VE = vec ? (int)(16 / esz) : 1;
+  // lanes per row of W: 32 bytes at least (vectors), more where two CTAs per SM remain, at most 256 bytes
+  int log_l = vec ? 1 : 3;
+  while (log_l < (vec ? 4 : 5) && (a.N + (VE << log_l) - 1) / (VE << log_l) > 2 * PLAN_SMS) ++log_l;
+  const unsigned blocks = (unsigned)((a.N + (VE << log_l) - 1) / (VE << log_l));
+  const RowsFn fn = dtype == ABS_FP32 ? (vec ? few_rows_fn<float, 4>(a.rows, a.act) : few_rows_fn<float, 1>(a.rows, a.act))
+                                      : (vec ? few_rows_fn<__nv_bfloat16, 8>(a.rows, a.act) : few_rows_fn<__nv_bfloat16, 1>(a.rows, a.act));
+  const int M = a.rows <= 2 ? (int)a.rows : a.rows <= 4 ? 4 : 8;
+  const size_t smem = (size_t)(small::NT / 32) * M * (VE << log_l) * 4;          // (at most 32 KB)
+  const cudaError_t e = launch(fn, dim3(blocks), small::NT, smem, 1, s, a, log_l);
+  return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
+}
+
+typedef void (*OutputsFn)(const small::Args, int, int);
+OutputsFn few_outputs_fn(int tiles, int act) {
+  return tiles == 1 ? ACT_FN(OutputsFn, small::few_outputs_kernel, act, 1) : ACT_FN(OutputsFn, small::few_outputs_kernel, act, 2);
+}
+int output_tiles(int N) { return N <= 8 ? 1 : 2; }
+size_t outputs_smem(int K, int N) {
+  const int t = output_tiles(N);
+  return (size_t)((K + 31) / 32) * t * 32 * 16 + (size_t)small::WARPS * 16 * (t * 8 + 1) * 4;
+}
+// Sizes for which that pass is faster than tiles of 128 x 64 (60000 rows: 256 -> 10 9.9 us against 18, 512 -> 10 16 against 21, 256 -> 16
+// 10.3 against 12.3, 512 -> 16 17.2 against 15.4); x has to be on 16 bytes.
+bool few_outputs_size(long long rows, int K, int N) { return N <= small::MAX_N && K <= (N % 8 ? 512 : 256) && rows >= 256 && K % 8 == 0; }
+int few_outputs(const small::Args& a, int sms, cudaStream_t s) {
+  const size_t smem = outputs_smem(a.K, a.N);            // (at most 25 KB)
+  const int groups = (int)((a.rows + 15) / 16);
+  const int per_sm = (int)((220 * 1024) / (smem + 1024)) < 4 ? (int)((220 * 1024) / (smem + 1024)) : 4;
+  const int blocks = (groups + small::WARPS - 1) / small::WARPS, most = sms * per_sm;
+  const cudaError_t e = launch(few_outputs_fn(output_tiles(a.N), a.act), dim3((unsigned)(blocks < most ? blocks : most)), small::WARPS * 32, smem, 1, s, a,
+                               (a.K + 31) / 32, groups);
+  return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
+}
+
 int check(long long rows, int n_in, int n_out, int act, int dtype) {
   if (dtype != ABS_FP32 && dtype != ABS_BF16_FP32MASTER) return fail(ABS_EUNSUPPORTED, "unknown dtype %d", dtype);
   if (act < ABS_ACT_NONE || act > ABS_ACT_SILU) return fail(ABS_EUNSUPPORTED, "unknown activation %d", act);
@@ -388,8 +501,10 @@ struct GradPlan { size_t dz, sums, x, w, part, total; long long ld_dz; int chunk
 GradPlan grad_plan(long long rows, int n_in, int n_out, int dtype, bool need_dz, bool pack_x, bool pack_w) {
   GradPlan g = {};
   const size_t esz = dtype == ABS_FP32 ? 4 : 2;
-  long long chunk = 64;
-  while ((rows + chunk - 1) / chunk > 128) chunk *= 2;
+  // rows whose column sums a CTA adds: enough CTAs for a few on every SM, at most 1024 chunks
+  const long long vecs = (n_out + 7) / 8, cols = (vecs + 63) / 64;
+  long long chunk = 32;
+  while ((rows + chunk - 1) / chunk > 1024 || (rows + chunk - 1) / chunk * cols > 16 * PLAN_SMS) chunk *= 2;
   g.chunk = (int)chunk;
   g.chunks = (int)((rows + chunk - 1) / chunk);
   g.ld_dz = (n_out + 7) / 8 * 8;
@@ -418,8 +533,11 @@ extern "C" int abs_linear_scratch_bytes(long long rows, int n_in, int n_out, int
   if (!out) return fail(ABS_EINVAL, "out is null");
   const int rc = check(rows, n_in, n_out, act, dtype);
   if (rc != ABS_OK) return rc;
-  const bool p = dtype != ABS_FP32 && !aligned;
-  *out = rows == 0 ? 0 : grad ? grad_plan(rows, n_in, n_out, dtype, act != ABS_ACT_NONE || p, p, p).total : fwd_plan(rows, n_in, n_out, dtype, p, p).total;
+  *out = 0;
+  if (rows == 0) return ABS_OK;
+  const bool bf16 = dtype != ABS_FP32, px = bf16 && !(aligned & 1), pw = bf16 && !(aligned & 2), pg = bf16 && !(aligned & 4);
+  if (grad) *out = grad_plan(rows, n_in, n_out, dtype, act != ABS_ACT_NONE || pg, px, pw).total;
+  else if (rows > few_rows_limit(dtype) && !(bf16 && !px && few_outputs_size(rows, n_in, n_out))) *out = fwd_plan(rows, n_in, n_out, dtype, px, pw).total;
   return ABS_OK;
 }
 
@@ -443,6 +561,8 @@ extern "C" int abs_linear(const void* x, long long ldx, const void* w, long long
   cudaStream_t s = (cudaStream_t)stream;
   int device, sms;
   if ((rc = current_device(&device, &sms)) != ABS_OK) return rc;
+  const small::Args sa = {x, w, bias, residual, y, pre, ldx, ldw, ldr, ldy, ldp, rows, n_in, n_out, act};
+  if (rows <= few_rows_limit(dtype)) return few_rows(sa, dtype, s);
   if (dtype == ABS_FP32) {
     fp32::Args p = {};
     p.a = (const float*)x; p.a_i = ldx; p.a_k = 1;
@@ -452,6 +572,7 @@ extern "C" int abs_linear(const void* x, long long ldx, const void* w, long long
     return fma_product(p, rows, n_out, n_in, act, device, s);
   }
   const bool pack_x = !tma_able(x, rows, ldx), pack_w = !tma_able(w, n_in, ldw);
+  if (!pack_x && few_outputs_size(rows, n_in, n_out)) return few_outputs(sa, sms, s);
   const FwdPlan f = fwd_plan(rows, n_in, n_out, dtype, pack_x, pack_w);
   if ((rc = check_scratch(scratch, scratch_bytes, f.total)) != ABS_OK) return rc;
   char* sc = (char*)scratch;
@@ -510,11 +631,18 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
   const bool with_dw = !bf16 && dw && db;              // the column sums come with the product
   float* part = db && !with_dw ? (float*)(sc + g.sums) : nullptr;
   cudaError_t e = cudaSuccess;
-  if (need_dz || part)
-    e = launch(dtype == ABS_FP32 ? slope_fn<float>(act) : slope_fn<__nv_bfloat16>(act), dim3((unsigned)((n_out + 31) / 32), (unsigned)g.chunks), 256, 0, 1, s,
-               dy, lddy, pre, ldp, need_dz ? (void*)(sc + g.dz) : (void*)nullptr, lddz, part, rows, n_out, g.chunk);
+  if (need_dz || part) {
+    SlopeArgs q = {dy, pre, need_dz ? (void*)(sc + g.dz) : (void*)nullptr, part, lddy, ldp, lddz, rows, n_out, g.chunk, 0, 0, Divisor()};
+    const bool vec = tma_able(dy, rows, lddy * (long long)esz / 2) && (act == ABS_ACT_NONE || tma_able(pre, rows, ldp * (long long)esz / 2)) &&
+                     (size_t)n_out * esz % 16 == 0;
+    const int VE = vec ? (int)(16 / esz) : 1, vecs = (n_out + VE - 1) / VE;
+    q.lv = vecs < 64 ? vecs : 64;
+    q.R = 256 / q.lv;
+    q.by_lv = Divisor((uint32_t)q.lv);
+    e = launch(slope_fn(dtype, vec, act), dim3((unsigned)((vecs + q.lv - 1) / q.lv), (unsigned)g.chunks), 256, 0, 1, s, q);
+  }
   if (part && e == cudaSuccess)
-    e = launch(dtype == ABS_FP32 ? column_kernel<float> : column_kernel<__nv_bfloat16>, dim3((unsigned)((n_out + 255) / 256)), 256, 0, 1, s,
+    e = launch(dtype == ABS_FP32 ? column_kernel<float> : column_kernel<__nv_bfloat16>, dim3((unsigned)((n_out + 31) / 32)), 256, 0, 1, s,
                (const float*)part, g.chunks, n_out, db);
   if (e != cudaSuccess) return fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
   if (!bf16) {

@@ -75,9 +75,21 @@ __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.comm
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// The box's rows to a matrix that TMA cannot address (row pitch or start not on 16 bytes): two columns per lane, row by row.
+// The box's rows to a matrix that TMA cannot address (row pitch or start not on 16 bytes, a ragged last column): two columns per lane,
+// row by row, or, where few columns are left, element by element over all rows.
 __device__ __forceinline__ void box_rows_out(const uint8_t* box, int lane, __nv_bfloat16* out, long long ld, int i0, int j0, int I, int J) {
-  const int rows = min(32, I - i0);
+  const int rows = min(32, I - i0), width = J - j0;
+  if (width <= 16) {
+    int r = lane / width, c = lane - r * width;
+    const int dr = 32 / width, dc = 32 - dr * width;
+    while (r < rows) {
+      out[(long long)(i0 + r) * ld + j0 + c] = *reinterpret_cast<const __nv_bfloat16*>(box + r * 128 + (((c >> 3) ^ (r & 7)) << 4) + ((c & 7) << 1));
+      r += dr;
+      c += dc;
+      if (c >= width) { c -= width; ++r; }
+    }
+    return;
+  }
   const int j = j0 + 2 * lane;
   for (int r = 0; r < rows; ++r) {
     const uint32_t w = *reinterpret_cast<const uint32_t*>(box + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + ((lane & 3) << 2));
