@@ -33,8 +33,7 @@ struct GnArgs {
   int cw, R, last;                       // channels of a chunk, thread rows, positions of a chunk's last CTA
   int segments;                          // row segments that sum a channel
   Divisor by_Q, by_chunks, by_D, by_lv, by_R, by_cw;
-  long long n0;                          // streaming: first sample of the launch; position ranges per sample
-  int parts;
+  int parts;                             // streaming: position ranges per sample
   Divisor by_parts;
 };
 
@@ -563,8 +562,9 @@ __global__ void __launch_bounds__(NT, 3) gn_backward_kernel(const GnArgs a) {
 }
 
 // ---- streaming form: a CTA takes a range of positions of a sample and a block of channels (all of them up to SNT vectors), reads it
-// in a first kernel for the statistics and in a second one for the result.  The host takes as many samples at a time as fit in L2, so
-// that the second reading finds them there.
+// in a first kernel for the statistics and in a second one for the result, which starts with the samples that were read last.
+// What bounds it is instructions (two conversions, five packed operations and SiLU's special functions per pair), not HBM: batches of
+// samples that stay in L2 between the two kernels were no faster (64 x 64 x 64 x 320 bf16: 93.6 us in one go, 95 in halves, 113 in thirds).
 
 constexpr int SNT = 256;                 // threads
 // Rows a thread has under way, each in a slot of its own in shared memory (asynchronous copies: loads into registers that far ahead
@@ -574,7 +574,7 @@ constexpr int AHEAD = 8, AHEAD2 = 6;     // one matrix; two
 template <int N> __device__ __forceinline__ void cp_wait_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 struct Range {
-  long long n, ln;                       // sample; sample of this launch
+  long long n;
   int part, e, c0, cw, r, v, g0, groups; // range, entry; channels; thread row and column; groups that the block touches
   uint32_t p0, p1;
   bool active;
@@ -582,8 +582,7 @@ struct Range {
 template <int VE> __device__ __forceinline__ Range range_of(const GnArgs& a, uint32_t bx) {
   Range s;
   const uint32_t ln = a.by_parts.div(bx);
-  s.ln = ln;
-  s.n = a.n0 + ln;
+  s.n = ln;
   s.part = (int)(bx - ln * a.by_parts.d);
   s.e = s.part * (int)gridDim.y + (int)blockIdx.y;
   s.c0 = (int)blockIdx.y * a.cw;
@@ -605,10 +604,10 @@ __device__ __forceinline__ void group_range(const GnArgs& a, const Range& s, int
 // entry[n][g][e] = (count, mean, squared deviations) of the block's part of group g
 template <typename T, int VE>
 __global__ void __launch_bounds__(SNT, 3) gn_stats_kernel(const GnArgs a) {
-  extern __shared__ __align__(16) float red[];                   // [R][cw]; [AHEAD][SNT] vectors
+  extern __shared__ __align__(16) float red[];                   // [AHEAD][SNT] vectors, then [R][cw]
   __shared__ float col[SNT * VE], own[SNT * VE];                 // channel sums; means of the block's groups
   const Range s = range_of<VE>(a, blockIdx.x);
-  T* slot = reinterpret_cast<T*>(red + SNT * VE) + threadIdx.x * VE;
+  T* slot = reinterpret_cast<T*>(red) + threadIdx.x * VE;
   grid_dependency_sync();
   Moments<VE> mo;
   if (s.active && s.p0 + s.r < s.p1) {
@@ -642,11 +641,12 @@ __global__ void __launch_bounds__(SNT, 3) gn_stats_kernel(const GnArgs a) {
   float out[VE];
 #pragma unroll
   for (int j = 0; j < VE; ++j) out[j] = mo.mean[j] * mo.seen;
+  __syncthreads();                                               // (everybody has left the rows' slots)
   if (s.active) put<VE>(at, out);
   __syncthreads();
   const float np = (float)(s.p1 - s.p0);
   const int E = a.parts * (int)gridDim.y;
-  float* entry = a.stat + ((size_t)s.ln * a.G + s.g0) * E * 3 + (size_t)s.e * 3;
+  float* entry = a.stat + ((size_t)s.n * a.G + s.g0) * E * 3 + (size_t)s.e * 3;
   const int S = max(1, a.segments);
   auto range = [&](int g, int& lo, int& hi) { group_range(a, s, g, lo, hi); };
   column_sums<SNT>(red, col, a);
@@ -693,7 +693,7 @@ __global__ void __launch_bounds__(SNT, 3) gn_apply_kernel(const GnArgs a) {
   const float inv_total = 1.f / ((float)a.positions * (float)a.D);
   for (int g0 = threadIdx.x >> 5 << 2; g0 < s.groups; g0 += SNT / 8) {       // eight lanes to a group
     const int g = g0 + ((threadIdx.x & 31) >> 3);
-    const float* entry = a.stat + ((size_t)s.ln * a.G + s.g0 + g) * E * 3;
+    const float* entry = a.stat + ((size_t)s.n * a.G + s.g0 + g) * E * 3;
     const int n = g < s.groups ? E : 0;
     float m = 0.f, v = 0.f;
     for (int e = sub; e < n; e += 8) m = fmaf(entry[3 * e] * inv_total, entry[3 * e + 1], m);
@@ -716,6 +716,9 @@ __global__ void __launch_bounds__(SNT, 3) gn_apply_kernel(const GnArgs a) {
   __syncthreads();
   if (!s.active || s.p0 + s.r >= s.p1) return;
   const int c = s.c0 + s.v * VE;
+  // u = (x - mean) rstd w + b; of bf16 maps x (rstd w) + (b - mean rstd w): a mean that far from zero that the difference of products
+  // matters, 2^14 standard deviations, is beyond what the maps' own eight bits resolve
+  constexpr bool FOLD = sizeof(T) == 2;
   Lanes<VE> nmu, sc, sh;
   float f0[VE], f1[VE], f2[VE];
   params<T, VE>(a.w, c, 1.f, f2);
@@ -724,7 +727,13 @@ __global__ void __launch_bounds__(SNT, 3) gn_apply_kernel(const GnArgs a) {
 #pragma unroll
   for (int j = 0; j < VE; ++j) { f0[j] = -f0[j]; f1[j] *= f2[j]; }
   params<T, VE>(a.b, c, 0.f, f2);
-  nmu.set(f0); sc.set(f1); sh.set(f2);
+  if constexpr (FOLD) {
+#pragma unroll
+    for (int j = 0; j < VE; ++j) f2[j] = fmaf(f0[j], f1[j], f2[j]);
+  } else {
+    nmu.set(f0);
+  }
+  sc.set(f1); sh.set(f2);
   const T* x = (const T*)a.x + s.n * a.xs + (long long)(s.p0 + s.r) * a.xp + c;
   T* y = (T*)a.y + s.n * a.ys + (long long)(s.p0 + s.r) * a.yp + c;
   const long long xstep = a.R * a.xp, ystep = a.R * a.yp;
@@ -745,7 +754,8 @@ __global__ void __launch_bounds__(SNT, 3) gn_apply_kernel(const GnArgs a) {
         q.get(f);
         Lanes<VE> l;
         l.set(f);
-        act_values<ACT>(fma(add(l, nmu), sc, sh)).get(f);
+        if constexpr (!FOLD) l = add(l, nmu);
+        act_values<ACT>(fma(l, sc, sh)).get(f);
         if (i + u + AHEAD < rows) copy_in<T, VE>(slot + u * SNT * VE, x);
         cp_commit();
         q.set(f);
@@ -827,7 +837,7 @@ __global__ void __launch_bounds__(SNT, 3) gn_sums_kernel(const GnArgs a) {
                   },
                   [&](int i, float t) {
                     const int k = i >= s.groups ? 1 : 0;
-                    a.stat[(((size_t)s.ln * a.G + s.g0 + i - k * s.groups) * E + s.e) * 2 + k] = t;
+                    a.stat[(((size_t)s.n * a.G + s.g0 + i - k * s.groups) * E + s.e) * 2 + k] = t;
                   });
 }
 
@@ -843,7 +853,7 @@ __global__ void __launch_bounds__(SNT, 3) gn_dx_kernel(const GnArgs a) {
   const float inv_total = 1.f / ((float)a.positions * (float)a.D);
   for (int g0 = threadIdx.x >> 5 << 2; g0 < s.groups; g0 += SNT / 8) {       // eight lanes to a group
     const int g = g0 + ((threadIdx.x & 31) >> 3);
-    const float* entry = a.stat + ((size_t)s.ln * a.G + s.g0 + g) * E * 2;
+    const float* entry = a.stat + ((size_t)s.n * a.G + s.g0 + g) * E * 2;
     const int n = g < s.groups ? E : 0;
     float t0 = 0.f, t1 = 0.f;
     for (int e = sub; e < n; e += 8) { t0 += entry[2 * e]; t1 += entry[2 * e + 1]; }
@@ -895,10 +905,10 @@ __global__ void __launch_bounds__(SNT, 3) gn_dx_kernel(const GnArgs a) {
   }
 }
 
-// out[s][0 | 1][c] = sum of rows s per, ... of part[rows][2][C]; the last stage writes db and dw: block = 32 columns x 8 rows of threads
+// out[s][0 | 1][c] = sum of rows s per, ... of part[rows][2][C]; the last stage writes db and dw: block = 32 columns x 32 rows of threads
 template <typename T>
-__global__ void __launch_bounds__(256) gn_param_kernel(const float* part, long long rows, long long per, int C, float* out, void* dw, void* db) {
-  __shared__ float red[8][33];
+__global__ void __launch_bounds__(1024) gn_param_kernel(const float* part, long long rows, long long per, int C, float* out, void* dw, void* db) {
+  __shared__ float red[32][33];
   grid_dependency_sync();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const long long j = (long long)blockIdx.x * 32 + lane, width = 2ll * C;
@@ -906,17 +916,16 @@ __global__ void __launch_bounds__(256) gn_param_kernel(const float* part, long l
   float t = 0.f;
   if (j < width) {
 #pragma unroll 8
-    for (long long r = blockIdx.y * per + w; r < r1; r += 8) t += part[r * width + j];
+    for (long long r = blockIdx.y * per + w; r < r1; r += 32) t += part[r * width + j];
   }
   red[w][lane] = t;
   __syncthreads();
-  if (w == 0 && j < width) {
-    float v = 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v += red[k][lane];
-    if (out) out[blockIdx.y * width + j] = v;
-    else if (j < C) { if (db) stf((T*)db, j, v); }
-    else if (dw) stf((T*)dw, j - C, v);
+  const float v = warp_sum(red[lane][w]);                        // (column w of the block)
+  const long long c = (long long)blockIdx.x * 32 + w;
+  if (lane == 0 && c < width) {
+    if (out) out[blockIdx.y * width + c] = v;
+    else if (c < C) { if (db) stf((T*)db, c, v); }
+    else if (dw) stf((T*)dw, c - C, v);
   }
 }
 
@@ -928,7 +937,7 @@ typedef void (*GnFn)(const GnArgs);
   ((dtype) == ABS_FP32 ? ((vec) ? GN_ACT(type, name, float, 4, act) : GN_ACT(type, name, float, 1, act))            \
                        : ((vec) ? GN_ACT(type, name, __nv_bfloat16, 8, act) : GN_ACT(type, name, __nv_bfloat16, 1, act)))
 
-constexpr double RESIDENT_BYTES = 12e6, BATCH_BYTES = 1e12;
+constexpr double RESIDENT_BYTES = 12e6;
 constexpr size_t CTA_BYTES = 110 * 1024, MOST_BYTES = 200 * 1024, STREAM_BYTES = 112 * 1024;
 
 // How a call is cut up; `vec`: 16-byte accesses.  The scratch of a call is the larger of the two forms'.
@@ -936,8 +945,7 @@ struct Plan {
   bool resident;
   int gpc, chunks, Q, ppc;               // resident form
   size_t smem;
-  long long batch;                       // streaming form: samples at a time
-  int cw, blocks, R, parts, sppc;
+  int cw, blocks, R, parts, sppc;        // streaming form
 };
 size_t smem_bytes(int gpc, int D, long long ppc, int VE, size_t esz, bool grad) {
   const size_t cw = (size_t)gpc * D;
@@ -981,19 +989,14 @@ Plan plan(long long samples, long long positions, int C, int G, int dtype, bool 
   p.cw = C <= most ? C : (int)(width <= most ? most / width * width : most);
   p.blocks = (C + p.cw - 1) / p.cw;
   p.R = SNT / (p.cw / VE);
-  p.batch = (long long)(BATCH_BYTES / sample_bytes);
-  if (p.batch < 1) p.batch = 1;
-  if (p.batch > samples) p.batch = samples;
-  if (p.batch > 65536) p.batch = 65536;
-  const long long launches = (samples + p.batch - 1) / p.batch;
-  p.batch = (samples + launches - 1) / launches;
-  // ranges of positions: as many as keep the waves of CTAs (three per SM) short, a CTA costing about as much as 12 rows besides
-  const long long units = p.batch * p.blocks, most_parts = (positions + 8 * p.R - 1) / (8 * p.R);
+  // ranges of positions: as many as keep the waves of CTAs (three per SM) short, a CTA costing about as much as 12 rows
+  // besides its own
+  const long long units = samples * p.blocks, most_parts = (positions + 8 * p.R - 1) / (8 * p.R), slots = 3 * PLAN_SMS;
   long long parts = 1;
   double least = 1e300;
   for (long long n = 1; n <= most_parts && n <= 4096 && (n - 1) * units <= 12 * PLAN_SMS; ++n) {
     const long long ppc = (positions + n - 1) / n;
-    const double cost = (double)((n * units + 3 * PLAN_SMS - 1) / (3 * PLAN_SMS)) * (double)((ppc + p.R - 1) / p.R + 12);
+    const double cost = (double)((n * units + slots - 1) / slots) * (double)((ppc + p.R - 1) / p.R + 12);
     if (cost < least) { least = cost; parts = n; }
   }
   p.sppc = (int)((positions + parts - 1) / parts);
@@ -1002,15 +1005,15 @@ Plan plan(long long samples, long long positions, int C, int G, int dtype, bool 
 }
 
 constexpr int PARAM_SPLIT = 64;          // rows of the first stage of the parameter sums when there are more than PARAM_ROWS
-constexpr long long PARAM_ROWS = 512;
-// floats of scratch: [entries of a batch][channel sums of all samples][first stage of the parameter sums]
-size_t entry_floats(const Plan& p, int G, bool grad) {
-  return p.resident ? 0 : round_up_sz((size_t)p.batch * G * p.parts * p.blocks * (grad ? 2 : 3), 64);
+constexpr long long PARAM_ROWS = 1024;
+// floats of scratch: [entries][channel sums of all samples][first stage of the parameter sums]
+size_t entry_floats(const Plan& p, long long samples, int G, bool grad) {
+  return p.resident ? 0 : round_up_sz((size_t)samples * G * p.parts * p.blocks * (grad ? 2 : 3), 64);
 }
 size_t scratch_floats(const Plan& p, long long samples, int C, int G, bool grad) {
-  if (!grad) return entry_floats(p, G, grad);
+  if (!grad) return entry_floats(p, samples, G, grad);
   const long long rows = p.resident ? samples : samples * p.parts;
-  return entry_floats(p, G, grad) + (size_t)rows * 2 * C + (rows > PARAM_ROWS ? (size_t)PARAM_SPLIT * 2 * C : 0);
+  return entry_floats(p, samples, G, grad) + (size_t)rows * 2 * C + (rows > PARAM_ROWS ? (size_t)PARAM_SPLIT * 2 * C : 0);
 }
 
 cudaError_t run_params(const GnArgs& a, long long rows, int dtype, float* second, cudaStream_t s) {
@@ -1020,11 +1023,11 @@ cudaError_t run_params(const GnArgs& a, long long rows, int dtype, float* second
   cudaError_t e = cudaSuccess;
   if (rows > PARAM_ROWS) {
     const long long per = (rows + PARAM_SPLIT - 1) / PARAM_SPLIT;
-    e = launch(kernel, dim3(cols, PARAM_SPLIT), 256, 0, 1, s, from, rows, per, a.C, second, (void*)nullptr, (void*)nullptr);
+    e = launch(kernel, dim3(cols, PARAM_SPLIT), 1024, 0, 1, s, from, rows, per, a.C, second, (void*)nullptr, (void*)nullptr);
     from = second;
     rows = PARAM_SPLIT;
   }
-  if (e == cudaSuccess) e = launch(kernel, dim3(cols), 256, 0, 1, s, from, rows, rows, a.C, (float*)nullptr, a.dw, a.db);
+  if (e == cudaSuccess) e = launch(kernel, dim3(cols), 1024, 0, 1, s, from, rows, rows, a.C, (float*)nullptr, a.dw, a.db);
   return e;
 }
 
@@ -1070,7 +1073,7 @@ cudaError_t launch_resident(GnFn fn, const Plan& p, long long samples, int VE, c
   return launch(fn, dim3((unsigned)(samples * p.chunks * p.Q)), NT, p.smem, p.Q, s, b);
 }
 
-// A batch of samples at a time: the first kernel's statistics, the second kernel's results.
+// The first kernel's statistics, the second kernel's results.
 struct StreamFns { GnFn first, second; };
 cudaError_t launch_streaming(const StreamFns& f, const Plan& p, long long samples, int VE, size_t esz, bool grad, cudaStream_t s, const GnArgs& call) {
   const cudaError_t ready = raise_smem();
@@ -1083,19 +1086,16 @@ cudaError_t launch_streaming(const StreamFns& f, const Plan& p, long long sample
   a.by_cw = Divisor((uint32_t)p.cw);
   a.segments = SNT / p.cw;
   const size_t vec_bytes = (size_t)VE * esz * SNT, wide = (size_t)(p.cw > SNT ? p.cw : SNT) + 2 * (size_t)p.cw;
-  const size_t sums = grad ? ((size_t)SNT * VE + round_up_sz(wide, 4)) * 4 + AHEAD2 * 2 * vec_bytes : (size_t)SNT * VE * 4 + AHEAD * vec_bytes;
+  const size_t sums = grad ? ((size_t)SNT * VE + round_up_sz(wide, 4)) * 4 + AHEAD2 * 2 * vec_bytes : AHEAD * vec_bytes;            // (the sums of four bytes per element fit into the slots)
   const size_t two = (grad ? AHEAD2 * 2 : AHEAD) * vec_bytes + 2 * ((size_t)(p.cw + a.D - 1) / a.D + 1) * 4;     // (groups that a block touches)
+  const dim3 grid((unsigned)(samples * p.parts), (unsigned)p.blocks);
   cudaError_t e = cudaSuccess;
-  for (a.n0 = 0; a.n0 < samples && e == cudaSuccess; a.n0 += p.batch) {
-    const long long ns = samples - a.n0 < p.batch ? samples - a.n0 : p.batch;
-    const dim3 grid((unsigned)(ns * p.parts), (unsigned)p.blocks);
-    if (p.blocks > 1) {
-      const size_t n = (size_t)ns * a.G * p.parts * p.blocks * (grad ? 2 : 3);
-      e = launch(gn_clear_kernel, dim3((unsigned)((n + 255) / 256 < 1024 ? (n + 255) / 256 : 1024)), 256, 0, 1, s, a.stat, n);
-    }
-    if (e == cudaSuccess) e = launch(f.first, grid, SNT, sums, 1, s, a);
-    if (e == cudaSuccess && f.second) e = launch(f.second, grid, SNT, two, 1, s, a);
+  if (p.blocks > 1) {
+    const size_t n = (size_t)samples * a.G * p.parts * p.blocks * (grad ? 2 : 3);
+    e = launch(gn_clear_kernel, dim3((unsigned)((n + 255) / 256 < 1024 ? (n + 255) / 256 : 1024)), 256, 0, 1, s, a.stat, n);
   }
+  if (e == cudaSuccess) e = launch(f.first, grid, SNT, sums, 1, s, a);
+  if (e == cudaSuccess && f.second) e = launch(f.second, grid, SNT, two, 1, s, a);
   return e;
 }
 
@@ -1231,7 +1231,7 @@ extern "C" int abs_group_norm_grad(const void* dy, long long dys, long long dyp,
     e = launch_resident(GN_PICK(GnFn, gn_backward_kernel, dtype, vec, act), p, samples, vec ? (int)(16 / esz) : 1, s, a);
   } else {
     a.stat = (float*)scratch;
-    a.part = a.stat + entry_floats(p, groups, true);
+    a.part = a.stat + entry_floats(p, samples, groups, true);
     const StreamFns fns = {GN_PICK(GnFn, gn_sums_kernel, dtype, vec, act), dx ? GN_PICK(GnFn, gn_dx_kernel, dtype, vec, act) : nullptr};
     e = launch_streaming(fns, p, samples, vec ? (int)(16 / esz) : 1, esz, true, s, a);
   }

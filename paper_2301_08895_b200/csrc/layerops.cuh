@@ -177,25 +177,41 @@ template <int N> __device__ __forceinline__ Lanes<N> fma(const Lanes<N>& a, cons
     for (int i = 0; i < N / 2; ++i) asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.p[i]) : "l"(a.p[i]), "l"(b.p[i]), "l"(c.p[i]));
   return r;
 }
-// 1 / (1 + exp(-z)) and so on, value by value; the products around them in pairs
+// 1 / (1 + exp(-z)) of N values.  Two values share a reciprocal, 1 / a = b / (a b): a value then costs the special-function unit one
+// and a half instructions instead of two, which bounds a pass of SiLU over bf16 (64 x 64 x 64 x 320: 63.6 -> @APPLY@ us).
+// exp(-z) stops at 2^60, so that the product of two stays finite: below z = -41.6 the result is 2^-60 instead of less.
+template <int N> __device__ __forceinline__ Lanes<N> sigmoids(const Lanes<N>& z) {
+  static_assert(N % 4 == 0, "pairs of pairs");
+  float v[N];
+  Lanes<N> k, one, a;
+  k.fill(-1.4426950408889634f);
+  one.fill(1.f);
+  mul(z, k).get(v);
+#pragma unroll
+  for (int j = 0; j < N; ++j) v[j] = ex2_approx(fminf(v[j], 60.f));
+  a.set(v);
+  a = add(a, one);
+  Lanes<N> r;
+#pragma unroll
+  for (int i = 0; i < N / 2; i += 2) {
+    Lanes<2> x, y, q;
+    float w[2];
+    x.p[0] = a.p[i];
+    y.p[0] = a.p[i + 1];
+    mul(x, y).get(w);
+    w[0] = rcp_approx(w[0]);
+    w[1] = rcp_approx(w[1]);
+    q.set(w);
+    r.p[i] = mul(q, y).p[0];
+    r.p[i + 1] = mul(q, x).p[0];
+  }
+  return r;
+}
 template <int ACT, int N> __device__ __forceinline__ Lanes<N> act_values(const Lanes<N>& z) {
   if constexpr (ACT == ABS_ACT_NONE) return z;
+  if constexpr (ACT == ABS_ACT_SILU && N > 1) return mul(z, sigmoids(z));
   float v[N];
   Lanes<N> r;
-  if constexpr (ACT == ABS_ACT_SILU) {
-    Lanes<N> k, one;
-    k.fill(-1.4426950408889634f);
-    one.fill(1.f);
-    mul(z, k).get(v);
-#pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = ex2_approx(v[j]);
-    r.set(v);
-    add(r, one).get(v);
-#pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = rcp_approx(v[j]);
-    r.set(v);
-    return mul(z, r);
-  }
   z.get(v);
 #pragma unroll
   for (int j = 0; j < N; ++j) v[j] = act_value<ACT>(v[j]);
@@ -203,23 +219,15 @@ template <int ACT, int N> __device__ __forceinline__ Lanes<N> act_values(const L
   return r;
 }
 template <int ACT, int N> __device__ __forceinline__ Lanes<N> act_slopes(const Lanes<N>& z) {
-  float v[N];
-  Lanes<N> r;
-  if constexpr (ACT == ABS_ACT_SILU) {
-    Lanes<N> k, one, minus, s;
-    k.fill(-1.4426950408889634f);
+  if constexpr (ACT == ABS_ACT_SILU && N > 1) {
+    Lanes<N> one, minus;
     one.fill(1.f);
     minus.fill(-1.f);
-    mul(z, k).get(v);
-#pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = ex2_approx(v[j]);
-    s.set(v);
-    add(s, one).get(v);
-#pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = rcp_approx(v[j]);
-    s.set(v);
+    const Lanes<N> s = sigmoids(z);
     return mul(s, fma(z, fma(s, minus, one), one));
   }
+  float v[N];
+  Lanes<N> r;
   z.get(v);
 #pragma unroll
   for (int j = 0; j < N; ++j) v[j] = act_slope<ACT>(v[j]);
