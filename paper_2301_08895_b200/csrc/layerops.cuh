@@ -178,7 +178,7 @@ template <int N> __device__ __forceinline__ Lanes<N> fma(const Lanes<N>& a, cons
   return r;
 }
 // 1 / (1 + exp(-z)) of N values.  Two values share a reciprocal, 1 / a = b / (a b): a value then costs the special-function unit one
-// and a half instructions instead of two, which bounds a pass of SiLU over bf16 (64 x 64 x 64 x 320: 63.6 -> @APPLY@ us).
+// and a half instructions instead of two, which bounds a pass of SiLU over bf16 (64 x 64 x 64 x 320: 63.6 -> 55.6 us).
 // exp(-z) stops at 2^60, so that the product of two stays finite: below z = -41.6 the result is 2^-60 instead of less.
 template <int N> __device__ __forceinline__ Lanes<N> sigmoids(const Lanes<N>& z) {
   static_assert(N % 4 == 0, "pairs of pairs");

@@ -47,7 +47,7 @@ namespace {
 constexpr int BK_TERMS = tc::BK;
 
 // dz = dy act'(pre), rounded to storage, and the column sums of the unrounded dz over each chunk of rows: one pass at HBM's pace
-// (8192 x 4096 bf16 GELU: @SLOPE@).  A thread takes VE columns of every R-th row, eight rows' loads under way.
+// (8192 x 4096 bf16 GELU: 201 MB in 40 us).  A thread takes VE columns of every R-th row, eight rows' loads under way.
 struct SlopeArgs {
   const void* dy; const void* pre; void* dz; float* part;
   long long lddy, ldp, lddz, rows;
@@ -160,14 +160,19 @@ __global__ void __launch_bounds__(256) finish_kernel(FinishArgs a) {
       s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
     }
     const float z[4] = {s.x, s.y, s.z, s.w};
+    float bias[4], res[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {                        // (all loads in front of the stores, which may alias them)
+      const bool in = (int)j + e < a.J;
+      bias[e] = a.bias && in ? __bfloat162float(a.bias[j + e]) : 0.f;
+      res[e] = a.res && in ? __bfloat162float(a.res[(long long)i * a.ldr + j + e]) : 0.f;
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if ((int)j + e >= a.J) break;
-      const float v = z[e] + (a.bias ? __bfloat162float(a.bias[j + e]) : 0.f);
+      const float v = z[e] + bias[e];
       if (a.pre) a.pre[(long long)i * a.ldp + j + e] = __float2bfloat16_rn(v);
-      float y = act_value<ACT>(v);
-      if (a.res) y += __bfloat162float(a.res[(long long)i * a.ldr + j + e]);
-      a.out[(long long)i * a.ldo + j + e] = __float2bfloat16_rn(y);
+      a.out[(long long)i * a.ldo + j + e] = __float2bfloat16_rn(act_value<ACT>(v) + res[e]);
     }
   }
 }
@@ -369,20 +374,23 @@ int pack(const void* src, long long rows, long long cols, long long ld, void* ds
 // ------------------------------------------------------------------ fp32 products
 
 struct FmaPlan { int bm, Q, kb_per; };
-// 64 x 64 or 128 x 128 tiles, and how many CTAs share a tile's sum.  A block of 32 k takes a CTA that is alone on its SM 1.2 or 3.4
-// us, two of them together 2.6 or 5.8 us (4096^3: 53 TFLOP/s); joining CTAs costs about a microsecond.
-FmaPlan plan_fma(long long I, int J, int K) {
+// 64 x 64 or 128 x 128 tiles, and how many CTAs share a tile's sum.  A block of 32 k takes a CTA that is alone on its SM 0.95 or 3.3
+// us, two of them together 1.7 or 5.8 us (4096^3: 54 TFLOP/s); joining CTAs costs about a microsecond.  CLUSTERS: clusters of q CTAs,
+// two per SM, that the GPU runs at a time (one more than that takes a second round: 72 clusters of four 150 us, pairs 126).  Rows that
+// do not start on 16 bytes (lines = false) cost the small tile another microsecond for two CTAs' block: their copies touch a line more.
+FmaPlan plan_fma(long long I, int J, int K, bool lines) {
+  static const int CLUSTERS[9] = {0, 296, 148, 93, 71, 56, 45, 37, 33};
   FmaPlan best = {};
   double least = 1e300;
   const int n_kb = (K + fp32::BK - 1) / fp32::BK;
   for (int bm : {64, 128}) {
     const long long tiles = (I + bm - 1) / bm * ((J + bm - 1) / bm);
-    const double one = bm == 64 ? 1.2 : 3.4, two = bm == 64 ? 2.6 : 5.8;
+    const double one = bm == 64 ? (lines ? 0.95 : 1.4) : 3.3, two = bm == 64 ? (lines ? 1.7 : 2.8) : 5.8;
     for (int q = 1; q <= 8 && q <= n_kb; ++q) {
       const int per = (n_kb + q - 1) / q;
       if ((q - 1) * per >= n_kb) continue;
-      const long long full = tiles * q / (2 * PLAN_SMS), rest = tiles * q - full * 2 * PLAN_SMS;
-      const double t = ((double)full * two + (rest > PLAN_SMS ? two : rest > 0 ? one : 0.0)) * per + (bm == 64 ? 2.0 : 4.0) + (q > 1 ? 1.0 : 0.0);
+      const long long full = tiles / CLUSTERS[q], rest = tiles - full * CLUSTERS[q];
+      const double t = ((double)full * two + (rest * q > PLAN_SMS - 12 ? two : rest > 0 ? one : 0.0)) * per + (bm == 64 ? 3.0 : 5.0) + (q > 1 ? 1.0 : 0.0);
       if (t < least) { least = t; best = FmaPlan{bm, q, per}; }
     }
   }
@@ -406,7 +414,8 @@ int fma_product(fp32::Args p, long long I, int J, int K, int act, int device, cu
   }
   for (long long pitch : {p.a_i, p.a_k, p.b_k, p.b_j})
     if (pitch > (1ll << 24)) return fail(ABS_EUNSUPPORTED, "fp32: row pitch %lld above 2^24", pitch);
-  const FmaPlan pl = plan_fma(I, J, K);
+  const bool lines = ((uintptr_t)p.a | (uintptr_t)p.b) % 16 == 0 && (p.a_i == 1 ? p.a_k : p.a_i) % 4 == 0 && (p.b_j == 1 ? p.b_k : p.b_j) % 4 == 0;
+  const FmaPlan pl = plan_fma(I, J, K, lines);
   p.I = (int)I; p.J = J; p.K = K;
   p.n_kb = (K + fp32::BK - 1) / fp32::BK;
   p.n_jt = (J + pl.bm - 1) / pl.bm;

@@ -14,7 +14,7 @@
 namespace absb {
 namespace fp32 {
 
-constexpr int NT = 256, BK = 32, STAGES = 3;
+constexpr int NT = 256, BK = 32;
 
 struct Args {
   const float* a; const float* b;
@@ -29,9 +29,11 @@ struct Args {
 
 template <int BM, int BN> struct Cfg {
   static constexpr int LDA = BM + 4, LDB = BN + 4;       // (4 modulo 32; with the swizzle no bank is hit twice, or twice at most)
+  static constexpr int STAGES = 3;
   static constexpr int KG = NT / ((BM / 8) * (BN / 8));
   static constexpr int STAGE = BK * (LDA + LDB);
-  static constexpr size_t SMEM = (size_t)STAGES * STAGE * 4;
+  static constexpr int RING = STAGES * STAGE, PARTS = KG * BM * BN + BN;           // floats: stages; the groups' sums, column sums
+  static constexpr size_t SMEM = (size_t)(RING > PARTS ? RING : PARTS) * 4;
 };
 
 __device__ __forceinline__ float ld_peer(const float* p, int rank) {
@@ -111,7 +113,7 @@ template <int W, bool B> struct Mover {
 template <int BM, int BN, int ACT>
 __global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Args p) {
   using C = Cfg<BM, BN>;
-  constexpr int KG = C::KG, KPG = BK / KG, TX = BN / 8;
+  constexpr int STAGES = C::STAGES, KG = C::KG, KPG = BK / KG, TX = BN / 8;
   extern __shared__ __align__(16) float sm[];
   const uint32_t tile = p.by_Q.div(blockIdx.x);
   const int rank = (int)(blockIdx.x - tile * p.by_Q.d);
@@ -132,8 +134,6 @@ __global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Args
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  for (int s = 0; s < STAGES - 1; ++s) fetch(s);
-
   const int g = (int)threadIdx.x / (NT / KG), t = (int)threadIdx.x % (NT / KG);
   const int tx = t % TX, ty = t / TX;
   layer::Lanes<2> acc[8][4];
@@ -143,10 +143,14 @@ __global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Args
     for (int v = 0; v < 4; ++v) acc[u][v].fill(0.f);
   float cs = 0.f;
   const bool sums = p.colsum != nullptr && it == 0 && (int)threadIdx.x < BN;
-  for (int kb = 0; kb < nkb; ++kb) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
-    __syncthreads();                     // the block is there, and everybody has left the one that is overwritten next
+#pragma unroll 1
+  for (int kb = 1 - STAGES; kb < nkb; ++kb) {                    // (the first steps only fetch: one copy of that code)
+    if (kb >= 0) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+      __syncthreads();                   // the block is there, and everybody has left the one that is overwritten next
+    }
     fetch(kb + STAGES - 1);
+    if (kb < 0) continue;
     const float* sa = sm + (kb % STAGES) * C::STAGE + g * KPG * C::LDA + 4 * ty;
     const float* sb = sm + (kb % STAGES) * C::STAGE + BK * C::LDA + g * KPG * C::LDB + 4 * tx;
     // eight k have one swizzle: with one group of threads it is known here, with four it is the group's and goes into row_of, col_of
@@ -180,31 +184,40 @@ __global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Args
   asm volatile("cp.async.wait_group 0;" ::: "memory");
   __syncthreads();
 
-  // groups of threads, then the CTAs of the cluster; the tile is left in sm[BM][BN]
+  // every group of threads leaves its sums, then all threads add them up (in place of the first group's): sm[BM][BN]
   float* tile_sm = sm;
-  float* cs_sm = sm + BM * BN;           // [BN]  (BM x BN + BN floats fit into the stages)
-  const int ga = KG == 1 ? 0 : swizzle_a(g * KPG), gb = KG == 1 ? 0 : swizzle_b(g * KPG) >> 1;
-  auto row_of = [&](int u) { return (u < 4 ? 0 : BM / 2) + ty * 4 + ((u & 3) ^ ga); };
-  auto col_of = [&](int v) { return (v < 2 ? 0 : BN / 2) + tx * 4 + 2 * ((v & 1) ^ gb); };
-#pragma unroll 1
-  for (int h = KG - 1; h >= 0; --h) {
-    if (g == h) {
+  float* cs_sm = sm + KG * BM * BN;      // [BN]
+  {
+    const int ga = KG == 1 ? 0 : swizzle_a(g * KPG), gb = KG == 1 ? 0 : swizzle_b(g * KPG) >> 1;
+    float* mine = sm + g * BM * BN + tx * 4;
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+    for (int u = 0; u < 8; ++u) {
+      float* row = mine + ((u < 4 ? 0 : BM / 2) + ty * 4 + ((u & 3) ^ ga)) * BN;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          unsigned long long* d = reinterpret_cast<unsigned long long*>(tile_sm + row_of(u) * BN + col_of(v));
-          if (h < KG - 1) {
-            layer::Lanes<2> o;
-            o.p[0] = *d;
-            acc[u][v] = layer::add(acc[u][v], o);
-          }
-          *d = acc[u][v].p[0];
-        }
+      for (int v = 0; v < 4; v += 2) {
+        layer::Lanes<4> q;
+        q.p[0] = gb ? acc[u][v + 1].p[0] : acc[u][v].p[0];
+        q.p[1] = gb ? acc[u][v].p[0] : acc[u][v + 1].p[0];
+        q.store(row + (v < 2 ? 0 : BN / 2));
+      }
     }
-    __syncthreads();
   }
   if (sums) cs_sm[threadIdx.x] = cs;
+  if (KG > 1) {
+    __syncthreads();
+#pragma unroll
+    for (int e = (int)threadIdx.x * 4; e < BM * BN; e += NT * 4) {
+      layer::Lanes<4> z;
+      z.load(sm + e);
+#pragma unroll
+      for (int h = 1; h < KG; ++h) {
+        layer::Lanes<4> o;
+        o.load(sm + h * BM * BN + e);
+        z = layer::add(z, o);
+      }
+      z.store(sm + e);
+    }
+  }
   if (p.Q > 1) {
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -213,26 +226,37 @@ __global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Args
     __syncthreads();
   }
   const int share = (BM + p.Q - 1) / p.Q, r0 = rank * share, r1 = min(min(BM, r0 + share), X);
-  for (int e = (int)threadIdx.x; e < (r1 - r0) * BN; e += NT) {
+  // a few elements at a time, all their loads in front of the first store (which the compiler has to take for an alias of theirs)
+  auto finish = [&](int e, const float z, float bias, float res) {
     const int r = r0 + e / BN, c = e % BN;
-    if (c >= Y) continue;
-    float z = 0.f;
-    if (p.Q > 1) {
-      float part[8];
-#pragma unroll
-      for (int q = 0; q < 8; ++q) part[q] = q < p.Q ? ld_peer(tile_sm + r * BN + c, q) : 0.f;
-#pragma unroll
-      for (int q = 0; q < 8; ++q) z += part[q];
-    } else {
-      z = tile_sm[r * BN + c];
-    }
     const long long i = i0 + r;
-    const int j = j0 + c;
-    if (p.bias) z += p.bias[j];
-    if (p.pre) p.pre[i * p.ldp + j] = z;
-    float y = layer::act_value<ACT>(z);
-    if (p.res) y += p.res[i * p.ldr + j];
-    p.out[i * p.ldo + j] = y;
+    const float v = z + bias;
+    if (p.pre) p.pre[i * p.ldp + j0 + c] = v;
+    p.out[i * p.ldo + j0 + c] = layer::act_value<ACT>(v) + res;
+  };
+  constexpr int U = 4;
+#pragma unroll 1
+  for (int e0 = (int)threadIdx.x; e0 < (r1 - r0) * BN; e0 += U * NT) {
+    float z[U], bias[U], res[U];
+    bool in[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int e = e0 + u * NT, r = r0 + e / BN, c = e % BN;
+      in[u] = r < r1 && c < Y;
+      z[u] = in[u] && p.Q == 1 ? tile_sm[r * BN + c] : 0.f;
+      bias[u] = in[u] && p.bias ? p.bias[j0 + c] : 0.f;
+      res[u] = in[u] && p.res ? p.res[(i0 + r) * p.ldr + j0 + c] : 0.f;
+    }
+    if (p.Q > 1) {
+#pragma unroll 4
+      for (int q = 0; q < p.Q; ++q)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (in[u]) z[u] += ld_peer(tile_sm + r0 * BN + e0 + u * NT, q);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (in[u]) finish(e0 + u * NT, z[u], bias[u], res[u]);
   }
   if (sums && rank == 0 && (int)threadIdx.x < Y) {
     float z = cs;

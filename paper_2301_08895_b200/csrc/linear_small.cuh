@@ -15,13 +15,16 @@ struct Args {
   int K, N, act;
 };
 
-// result of one output, from its sum over k
-template <typename T, int ACT> __device__ __forceinline__ void finish(const Args& a, long long m, int j, float z) {
-  if (a.bias) z += ldf((const T*)a.bias, j);
+// result of one output from its sum over k, in two halves: what is loaded, and what is stored.  (A store may alias a load for all the
+// compiler knows; several outputs' loads come first.)
+template <typename T> __device__ __forceinline__ void fetch(const Args& a, long long m, int j, float& bias, float& res) {
+  bias = a.bias ? ldf((const T*)a.bias, j) : 0.f;
+  res = a.res ? ldf((const T*)a.res, m * a.ldr + j) : 0.f;
+}
+template <typename T, int ACT> __device__ __forceinline__ void finish(const Args& a, long long m, int j, float z, float bias, float res) {
+  z += bias;
   if (a.pre) stf((T*)a.pre, m * a.ldp + j, z);
-  float y = layer::act_value<ACT>(z);
-  if (a.res) y += ldf((const T*)a.res, m * a.ldr + j);
-  stf((T*)a.y, m * a.ldy + j, y);
+  stf((T*)a.y, m * a.ldy + j, layer::act_value<ACT>(z) + res);
 }
 
 // ---- a few rows: a pass over W, whose bytes bound the call (or its latency).  L neighbouring lanes take L VE columns of
@@ -116,10 +119,11 @@ __global__ void __launch_bounds__(NT) few_rows_kernel(const Args a, int log_l) {
   for (int i = threadIdx.x; i < M * cols; i += NT) {
     const int m = i / cols, c = i - m * cols;
     if (m < a.rows && j0 + c < a.N) {
-      float z = 0.f;
+      float z = 0.f, bias, res;
+      fetch<T>(a, m, j0 + c, bias, res);
 #pragma unroll
       for (int q = 0; q < NT / 32; ++q) z += red[(q * M + m) * cols + c];
-      finish<T, ACT>(a, m, j0 + c, z);
+      finish<T, ACT>(a, m, j0 + c, z, bias, res);
     }
   }
 }
@@ -164,7 +168,7 @@ __global__ void __launch_bounds__(WARPS * 32) few_outputs_kernel(const Args a, i
     for (int t = 0; t < NTILES; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) c[t][e] = 0.f;
-    constexpr int U = 8;
+    constexpr int U = 4;                                         // (eight take registers from other CTAs and are no faster)
     for (int b = 0; b < n_blocks; b += U) {
       uint4 p0[U], p1[U];
       const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
@@ -199,7 +203,9 @@ __global__ void __launch_bounds__(WARPS * 32) few_outputs_kernel(const Args a, i
     int m = lane / a.N, j = lane - m * a.N;                      // element lane, lane + 32, ... of the group's results
     const int dm = 32 / a.N, dj = 32 - dm * a.N;
     while (m < n_rows) {
-      finish<__nv_bfloat16, ACT>(a, m0 + m, j, stage[m * P + j]);
+      float bias, res;
+      fetch<__nv_bfloat16>(a, m0 + m, j, bias, res);
+      finish<__nv_bfloat16, ACT>(a, m0 + m, j, stage[m * P + j], bias, res);
       m += dm;
       j += dj;
       if (j >= a.N) { j -= a.N; ++m; }
