@@ -372,6 +372,11 @@ int abs_group_norm_scratch_bytes(long long samples, long long positions, int cha
  * ABS_OK.  Synchronises the stream; operations on other streams are covered once they have completed. */
 int abs_op_status(void* stream);
 
+/* Test aid for that path: enqueues a one-warp kernel that waits, with these kernels' own wait routine and a limit of
+ * limit_us microseconds (1 .. 1000000), on a barrier that nothing ever signals.  The next abs_op_status on
+ * the stream is expected to return ABS_ETIMEOUT, and the one after it ABS_OK. */
+int abs_op_selftest_wait_timeout(int limit_us, void* stream);
+
 /* How the context runs (the paper has no counterpart): *partials = number of fp32 partial sums
  * the Eq. 3 step adds up per parameter (0: one per selected worker), *row_block = padding unit of
  * a version group's gradient rows, *rows_cap = row capacity of the activation buffers,

@@ -103,6 +103,7 @@ def lib():
         l.abs_group_norm_grad.argtypes = [p, q, q, p, q, q, p, p, p, p, p, q, q, p, p, q, q, i, i, i, i, p, z, p]
         l.abs_group_norm_scratch_bytes.argtypes = [q, q, i, i, i, i, C.POINTER(z)]
         l.abs_op_status.argtypes = [p]
+        l.abs_op_selftest_wait_timeout.argtypes = [i, p]
         l.abs_get_plan.argtypes = [C.c_void_p, C.POINTER(C.c_int), C.POINTER(C.c_int),
                                    C.POINTER(C.c_int), C.POINTER(C.c_int)]
         l.abs_profile_start.argtypes = [C.c_void_p, C.c_int]

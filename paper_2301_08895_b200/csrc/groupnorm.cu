@@ -353,10 +353,10 @@ __global__ void __launch_bounds__(NT, 3) gn_forward_kernel(const GnArgs a) {
   for (int j = 0; j < VE; ++j) out[j] = me[j] * seen;
   if (s.active) put<VE>(at, out);
   __syncthreads();
-  const float inv_cnt = 1.f / ((float)s.np * (float)a.D);
+  const float cnt = (float)s.np * (float)a.D;
   column_sums<NT>(red, col, a);
   __syncthreads();
-  group_sums<NT>(col, S, a.cw, s.groups, a.D, range, [&](int g, float t) { own[g] = t * inv_cnt; });
+  group_sums<NT>(col, S, a.cw, s.groups, a.D, range, [&](int g, float t) { own[g] = t / cnt; });
   __syncthreads();
   if (s.active) {
     float mu[VE];
@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(NT, 3) gn_forward_kernel(const GnArgs a) {
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
       const float e = me[j] - mu[j];
-      out[j] = fmaf(e * e, seen, mm[j]);
+      out[j] = seen > 0.f ? fmaf(e * e, seen, mm[j]) : 0.f;      // (a thread without rows: no 0 times infinity)
     }
     put<VE>(at, out);
   }
@@ -375,7 +375,8 @@ __global__ void __launch_bounds__(NT, 3) gn_forward_kernel(const GnArgs a) {
   if (a.Q > 1) { __syncwarp(); cluster_arrive(); cluster_wait(); }
   else __syncthreads();
   for (int g = threadIdx.x; g < s.groups; g += NT) {
-    // M = sum n_i m_i / N, V = sum (v_i + n_i (m_i - M)^2) / N; all CTAs but the last have the same count
+    // M = m_0 + sum n_i (m_i - m_0) / N (equal means stay what they are), V = sum (v_i + n_i (m_i - M)^2) / N; all CTAs but the last
+    // have the same count
     float pm[8], pv[8], M = 0.f, V = 0.f;
     const float inv_total = 1.f / (float)a.positions, n0 = (float)a.ppc * inv_total, n1 = (float)a.last * inv_total;
     const float inv_all = inv_total / (float)a.D;
@@ -387,9 +388,10 @@ __global__ void __launch_bounds__(NT, 3) gn_forward_kernel(const GnArgs a) {
         pv[q] = a.Q > 1 ? ld_peer(own + a.gpc + g, q) : own[a.gpc + g];
       }
     }
+    M = pm[0];
 #pragma unroll
-    for (int q = 0; q < 8; ++q)
-      if (q < a.Q) M = fmaf(q == a.Q - 1 ? n1 : n0, pm[q], M);
+    for (int q = 1; q < 8; ++q)
+      if (q < a.Q) M = fmaf(q == a.Q - 1 ? n1 : n0, pm[q] - pm[0], M);
 #pragma unroll
     for (int q = 0; q < 8; ++q)
       if (q < a.Q) {
@@ -665,7 +667,7 @@ __global__ void __launch_bounds__(SNT, 3) gn_stats_kernel(const GnArgs a) {
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
       const float e = mo.mean[j] - mu[j];
-      out[j] = fmaf(e * e, mo.seen, mo.dev[j]);
+      out[j] = mo.seen > 0.f ? fmaf(e * e, mo.seen, mo.dev[j]) : 0.f;      // (a thread without rows: no 0 times infinity)
     }
     put<VE>(at, out);
   }
@@ -695,9 +697,11 @@ __global__ void __launch_bounds__(SNT, 3) gn_apply_kernel(const GnArgs a) {
     const int g = g0 + ((threadIdx.x & 31) >> 3);
     const float* entry = a.stat + ((size_t)s.n * a.G + s.g0 + g) * E * 3;
     const int n = g < s.groups ? E : 0;
+    const int first = n > 0 ? s.e % (int)gridDim.y : 0;          // (an entry of this block: its range may be empty elsewhere)
+    const float m0 = n > 0 ? entry[3 * first + 1] : 0.f;
     float m = 0.f, v = 0.f;
-    for (int e = sub; e < n; e += 8) m = fmaf(entry[3 * e] * inv_total, entry[3 * e + 1], m);
-    m = eight_sum(m);
+    for (int e = sub; e < n; e += 8) m = fmaf(entry[3 * e] * inv_total, entry[3 * e + 1] - m0, m);
+    m = eight_sum(m) + m0;                                       // (relative to one of them: equal means stay what they are)
     for (int e = sub; e < n; e += 8) {
       const float d = entry[3 * e + 1] - m;
       v += fmaf(entry[3 * e] * d, d, entry[3 * e + 2]);
@@ -716,9 +720,6 @@ __global__ void __launch_bounds__(SNT, 3) gn_apply_kernel(const GnArgs a) {
   __syncthreads();
   if (!s.active || s.p0 + s.r >= s.p1) return;
   const int c = s.c0 + s.v * VE;
-  // u = (x - mean) rstd w + b; of bf16 maps x (rstd w) + (b - mean rstd w): a mean that far from zero that the difference of products
-  // matters, 2^14 standard deviations, is beyond what the maps' own eight bits resolve
-  constexpr bool FOLD = sizeof(T) == 2;
   Lanes<VE> nmu, sc, sh;
   float f0[VE], f1[VE], f2[VE];
   params<T, VE>(a.w, c, 1.f, f2);
@@ -727,12 +728,7 @@ __global__ void __launch_bounds__(SNT, 3) gn_apply_kernel(const GnArgs a) {
 #pragma unroll
   for (int j = 0; j < VE; ++j) { f0[j] = -f0[j]; f1[j] *= f2[j]; }
   params<T, VE>(a.b, c, 0.f, f2);
-  if constexpr (FOLD) {
-#pragma unroll
-    for (int j = 0; j < VE; ++j) f2[j] = fmaf(f0[j], f1[j], f2[j]);
-  } else {
-    nmu.set(f0);
-  }
+  nmu.set(f0);
   sc.set(f1); sh.set(f2);
   const T* x = (const T*)a.x + s.n * a.xs + (long long)(s.p0 + s.r) * a.xp + c;
   T* y = (T*)a.y + s.n * a.ys + (long long)(s.p0 + s.r) * a.yp + c;
@@ -754,8 +750,7 @@ __global__ void __launch_bounds__(SNT, 3) gn_apply_kernel(const GnArgs a) {
         q.get(f);
         Lanes<VE> l;
         l.set(f);
-        if constexpr (!FOLD) l = add(l, nmu);
-        act_values<ACT>(fma(l, sc, sh)).get(f);
+        act_values<ACT>(fma(add(l, nmu), sc, sh)).get(f);
         if (i + u + AHEAD < rows) copy_in<T, VE>(slot + u * SNT * VE, x);
         cp_commit();
         q.set(f);
@@ -1115,13 +1110,6 @@ int check(long long samples, long long positions, int channels, int groups, int 
   return ABS_OK;
 }
 
-int check_scratch(const void* scratch, size_t have, size_t need) {
-  if (need == 0) return ABS_OK;
-  if (have < need) return fail(ABS_ENOSPACE, "scratch holds %zu bytes, %zu needed", have, need);
-  if (!scratch || (uintptr_t)scratch % 256) return fail(ABS_EINVAL, "scratch is null or not 256-byte aligned");
-  return ABS_OK;
-}
-
 // maps [samples][positions][C] with pitches s, p
 int check_maps(const char* name, const void* ptr, long long s, long long p, long long samples, long long positions, int C, size_t esz) {
   if (!ptr) return fail(ABS_EINVAL, "%s is null", name);
@@ -1131,9 +1119,10 @@ int check_maps(const char* name, const void* ptr, long long s, long long p, long
   return ABS_OK;
 }
 
+Span flat(const void* ptr, long long bytes) { return Span{(uintptr_t)ptr, (uintptr_t)ptr + (ptr ? (uintptr_t)bytes : 0), 0, 0}; }
 Span maps_span(const void* ptr, long long s, long long p, long long samples, long long positions, int C, size_t esz) {
   Span r = {(uintptr_t)ptr, (uintptr_t)ptr, (long long)(p * (long long)esz), (long long)(C * (long long)esz)};
-  if (ptr) r.hi += (uintptr_t)(((samples - 1) * s + (positions - 1) * p + C) * (long long)esz);
+  if (ptr && samples > 0) r.hi += (uintptr_t)(((samples - 1) * s + (positions - 1) * p + C) * (long long)esz);
   if (samples > 1 && s % (p > 0 ? p : 1)) r.ld = 0;      // (rows of different samples are not a multiple of the pitch apart)
   return r;
 }
@@ -1162,9 +1151,15 @@ extern "C" int abs_group_norm(const void* x, long long xs, long long xp, const v
   const size_t esz = dtype == ABS_FP32 ? 4 : 2;
   if ((rc = check_maps("x", x, xs, xp, samples, positions, channels, esz)) != ABS_OK) return rc;
   if ((rc = check_maps("y", y, ys, yp, samples, positions, channels, esz)) != ABS_OK) return rc;
-  if (!(x == y && (samples == 1 || xs == ys) && (positions == 1 || xp == yp)) &&
-      overlap(maps_span(x, xs, xp, samples, positions, channels, esz), maps_span(y, ys, yp, samples, positions, channels, esz)))
-    return fail(ABS_EINVAL, "y overlaps x without being the same maps");
+  if ((rc = check_vector("w", w, esz)) != ABS_OK || (rc = check_vector("b", b, esz)) != ABS_OK) return rc;
+  if ((rc = check_vector("mean", mean, 4)) != ABS_OK || (rc = check_vector("rstd", rstd, 4)) != ABS_OK) return rc;
+  const Span sx = maps_span(x, xs, xp, samples, positions, channels, esz), sy = maps_span(y, ys, yp, samples, positions, channels, esz);
+  const Span sw = flat(w, channels * esz), sb = flat(b, channels * esz), sm = flat(mean, samples * groups * 4), sr = flat(rstd, samples * groups * 4);
+  if (!(x == y && (samples == 1 || xs == ys) && (positions == 1 || xp == yp)) && overlap(sx, sy)) return fail(ABS_EINVAL, "y overlaps x without being the same maps");
+  if (overlap(sy, sw) || overlap(sy, sb)) return fail(ABS_EINVAL, "y overlaps w or b");
+  if (overlap(sm, sr)) return fail(ABS_EINVAL, "mean overlaps rstd");
+  for (const Span& st : {sm, sr})
+    if (overlap(st, sx) || overlap(st, sy) || overlap(st, sw) || overlap(st, sb)) return fail(ABS_EINVAL, "mean or rstd overlaps another argument");
   GnArgs a = {};
   a.x = x; a.y = y; a.w = w; a.b = b; a.mean = mean; a.rstd = rstd;
   a.xs = xs; a.xp = xp; a.ys = ys; a.yp = yp;
@@ -1173,7 +1168,7 @@ extern "C" int abs_group_norm(const void* x, long long xs, long long xp, const v
   a.by_D = Divisor((uint32_t)a.D);
   const bool vec = (size_t)channels * esz % 16 == 0 && on16(x) && on16(y) && pitch16(samples, positions, xs, xp, esz) && pitch16(samples, positions, ys, yp, esz);
   const Plan p = plan(samples, positions, channels, groups, dtype, false, vec);
-  if ((rc = check_scratch(scratch, scratch_bytes, scratch_floats(p, samples, channels, groups, false) * 4)) != ABS_OK) return rc;
+  if ((rc = check_scratch(scratch, scratch_bytes, scratch_floats(p, samples, channels, groups, false) * 4, {sx, sy, sw, sb, sm, sr})) != ABS_OK) return rc;
   a.gpc = p.gpc; a.chunks = p.chunks; a.Q = p.Q; a.ppc = p.ppc;
   cudaStream_t s = (cudaStream_t)stream;
   cudaError_t e;
@@ -1196,21 +1191,29 @@ extern "C" int abs_group_norm_grad(const void* dy, long long dys, long long dyp,
   const size_t esz = dtype == ABS_FP32 ? 4 : 2;
   cudaError_t e = cudaSuccess;
   if (samples == 0 || positions == 0) {
+    if ((rc = check_vector("dw", dw, esz)) != ABS_OK || (rc = check_vector("db", db, esz)) != ABS_OK) return rc;
     if (dw) e = cudaMemsetAsync(dw, 0, channels * esz, (cudaStream_t)stream);
     if (db && e == cudaSuccess) e = cudaMemsetAsync(db, 0, channels * esz, (cudaStream_t)stream);
     return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "memset: %s", cudaGetErrorString(e));
   }
   if (!mean || !rstd) return fail(ABS_EINVAL, "mean and rstd of the forward pass are needed");
+  if ((rc = check_vector("dw", dw, esz)) != ABS_OK || (rc = check_vector("db", db, esz)) != ABS_OK) return rc;
   if ((rc = check_maps("dy", dy, dys, dyp, samples, positions, channels, esz)) != ABS_OK) return rc;
   if ((rc = check_maps("x", x, xs, xp, samples, positions, channels, esz)) != ABS_OK) return rc;
-  if (dx) {
-    if ((rc = check_maps("dx", dx, dxs, dxp, samples, positions, channels, esz)) != ABS_OK) return rc;
-    const Span sd = maps_span(dx, dxs, dxp, samples, positions, channels, esz);
-    if (overlap(sd, maps_span(x, xs, xp, samples, positions, channels, esz))) return fail(ABS_EINVAL, "dx overlaps x");
-    if (!(dx == dy && (samples == 1 || dxs == dys) && (positions == 1 || dxp == dyp)) &&
-        overlap(sd, maps_span(dy, dys, dyp, samples, positions, channels, esz)))
-      return fail(ABS_EINVAL, "dx overlaps dy without being the same maps");
-  }
+  if (dx && (rc = check_maps("dx", dx, dxs, dxp, samples, positions, channels, esz)) != ABS_OK) return rc;
+  if ((rc = check_vector("w", w, esz)) != ABS_OK || (rc = check_vector("b", b, esz)) != ABS_OK) return rc;
+  if ((rc = check_vector("mean", mean, 4)) != ABS_OK || (rc = check_vector("rstd", rstd, 4)) != ABS_OK) return rc;
+  const Span sx = maps_span(x, xs, xp, samples, positions, channels, esz), sg = maps_span(dy, dys, dyp, samples, positions, channels, esz);
+  const Span sd = maps_span(dx, dxs, dxp, dx ? samples : 0, positions, channels, esz), s1 = flat(dw, channels * esz), s2 = flat(db, channels * esz);
+  const Span fixed[4] = {flat(w, channels * esz), flat(b, channels * esz), flat(mean, samples * groups * 4), flat(rstd, samples * groups * 4)};
+  if (overlap(sd, sx)) return fail(ABS_EINVAL, "dx overlaps x");
+  if (!(dx == dy && (samples == 1 || dxs == dys) && (positions == 1 || dxp == dyp)) && overlap(sd, sg))
+    return fail(ABS_EINVAL, "dx overlaps dy without being the same maps");
+  if (overlap(s1, s2) || overlap(s1, sd) || overlap(s2, sd)) return fail(ABS_EINVAL, "two gradients overlap");
+  for (const Span& o : {sd, s1, s2})
+    for (const Span& f : fixed)
+      if (overlap(o, f)) return fail(ABS_EINVAL, "a gradient overlaps an operand");
+  if (overlap(s1, sx) || overlap(s1, sg) || overlap(s2, sx) || overlap(s2, sg)) return fail(ABS_EINVAL, "a gradient overlaps an operand");
   GnArgs a = {};
   a.x = x; a.dy = dy; a.y = dx; a.w = w; a.b = b; a.dw = dw; a.db = db;
   a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
@@ -1222,7 +1225,8 @@ extern "C" int abs_group_norm_grad(const void* dy, long long dys, long long dyp,
                    pitch16(samples, positions, dys, dyp, esz) && (!dx || pitch16(samples, positions, dxs, dxp, esz));
   const Plan p = plan(samples, positions, channels, groups, dtype, true, vec);
   if (!dx && !dw && !db) return ABS_OK;
-  if ((rc = check_scratch(scratch, scratch_bytes, scratch_floats(p, samples, channels, groups, true) * 4)) != ABS_OK) return rc;
+  if ((rc = check_scratch(scratch, scratch_bytes, scratch_floats(p, samples, channels, groups, true) * 4,
+                          {sx, sg, sd, s1, s2, fixed[0], fixed[1], fixed[2], fixed[3]})) != ABS_OK) return rc;
   a.gpc = p.gpc; a.chunks = p.chunks; a.Q = p.Q; a.ppc = p.ppc;
   cudaStream_t s = (cudaStream_t)stream;
   const long long rows = p.resident ? samples : samples * p.parts;

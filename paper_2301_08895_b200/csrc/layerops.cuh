@@ -2,6 +2,8 @@
 #pragma once
 #include <math.h>
 
+#include <initializer_list>
+
 #include "common.cuh"
 
 namespace absb {
@@ -64,6 +66,10 @@ inline bool overlap(const Span& a, const Span& b) {
   const long long d = (long long)((b.lo >= a.lo ? b.lo - a.lo : a.ld - (a.lo - b.lo) % a.ld) % a.ld);   // b's column offset from a
   return d < a.row || d + b.row > a.ld;
 }
+
+// Scratch: large enough, aligned, apart from the call's other memory; vectors: aligned to their type (linear.cu).
+int check_scratch(const void* scratch, size_t have, size_t need, std::initializer_list<Span> others);
+int check_vector(const char* name, const void* p, size_t esz);
 
 // ---- activations.  Exponential and reciprocal are the hardware's approximations (2^-22 each, denormal results are zero):
 // two instructions of the special-function unit per value, where expf and a division cost some twenty instructions.
@@ -179,16 +185,21 @@ template <int N> __device__ __forceinline__ Lanes<N> fma(const Lanes<N>& a, cons
 }
 // 1 / (1 + exp(-z)) of N values.  Two values share a reciprocal, 1 / a = b / (a b): a value then costs the special-function unit one
 // and a half instructions instead of two, which bounds a pass of SiLU over bf16 (64 x 64 x 64 x 320: 63.6 -> 55.6 us).
-// exp(-z) stops at 2^60, so that the product of two stays finite: below z = -41.6 the result is 2^-60 instead of less.
-template <int N> __device__ __forceinline__ Lanes<N> sigmoids(const Lanes<N>& z) {
+// z is held at -41.5 from below (a NaN stays one), so that the product of two values of 1 + exp(-z) <= 2^60 stays finite: where it is held,
+// SiLU and its slope, both below 4e-17, are those of -41.5.
+template <int N> __device__ __forceinline__ Lanes<N> sigmoids(const Lanes<N>& z, Lanes<N>& held) {
   static_assert(N % 4 == 0, "pairs of pairs");
   float v[N];
   Lanes<N> k, one, a;
   k.fill(-1.4426950408889634f);
   one.fill(1.f);
-  mul(z, k).get(v);
+  z.get(v);
 #pragma unroll
-  for (int j = 0; j < N; ++j) v[j] = ex2_approx(fminf(v[j], 60.f));
+  for (int j = 0; j < N; ++j) asm("max.NaN.f32 %0, %1, %2;" : "=f"(v[j]) : "f"(v[j]), "f"(-41.5f));
+  held.set(v);
+  mul(held, k).get(v);
+#pragma unroll
+  for (int j = 0; j < N; ++j) v[j] = ex2_approx(v[j]);
   a.set(v);
   a = add(a, one);
   Lanes<N> r;
@@ -209,7 +220,11 @@ template <int N> __device__ __forceinline__ Lanes<N> sigmoids(const Lanes<N>& z)
 }
 template <int ACT, int N> __device__ __forceinline__ Lanes<N> act_values(const Lanes<N>& z) {
   if constexpr (ACT == ABS_ACT_NONE) return z;
-  if constexpr (ACT == ABS_ACT_SILU && N > 1) return mul(z, sigmoids(z));
+  if constexpr (ACT == ABS_ACT_SILU && N > 1) {
+    Lanes<N> held;
+    const Lanes<N> s = sigmoids(z, held);
+    return mul(held, s);
+  }
   float v[N];
   Lanes<N> r;
   z.get(v);
@@ -223,8 +238,9 @@ template <int ACT, int N> __device__ __forceinline__ Lanes<N> act_slopes(const L
     Lanes<N> one, minus;
     one.fill(1.f);
     minus.fill(-1.f);
-    const Lanes<N> s = sigmoids(z);
-    return mul(s, fma(z, fma(s, minus, one), one));
+    Lanes<N> held;
+    const Lanes<N> s = sigmoids(z, held);
+    return mul(s, fma(held, fma(s, minus, one), one));
   }
   float v[N];
   Lanes<N> r;

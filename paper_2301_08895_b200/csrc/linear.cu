@@ -24,6 +24,20 @@ int fail(int code, const char* fmt, ...) {
   return code;
 }
 
+int check_scratch(const void* scratch, size_t have, size_t need, std::initializer_list<Span> others) {
+  if (need == 0) return ABS_OK;
+  if (have < need) return fail(ABS_ENOSPACE, "scratch holds %zu bytes, %zu needed", have, need);
+  if (!scratch || (uintptr_t)scratch % 256) return fail(ABS_EINVAL, "scratch is null or not 256-byte aligned");
+  const Span mine = {(uintptr_t)scratch, (uintptr_t)scratch + need, 0, 0};
+  for (const Span& o : others)
+    if (overlap(mine, o)) return fail(ABS_EINVAL, "scratch overlaps an operand or a result");
+  return ABS_OK;
+}
+
+int check_vector(const char* name, const void* p, size_t esz) {
+  return p && (uintptr_t)p % esz ? fail(ABS_EINVAL, "%s is not aligned to its type", name) : ABS_OK;
+}
+
 int current_device(int* device, int* sms) {
   static std::atomic<int> known[MAX_DEVICES];
   cudaError_t e = cudaGetDevice(device);
@@ -529,12 +543,6 @@ GradPlan grad_plan(long long rows, int n_in, int n_out, int dtype, bool need_dz,
   return g;
 }
 
-int check_scratch(const void* scratch, size_t have, size_t need) {
-  if (need == 0) return ABS_OK;
-  if (have < need) return fail(ABS_ENOSPACE, "scratch holds %zu bytes, %zu needed", have, need);
-  if (!scratch || (uintptr_t)scratch % 256) return fail(ABS_EINVAL, "scratch is null or not 256-byte aligned");
-  return ABS_OK;
-}
 
 }  // namespace
 
@@ -562,6 +570,9 @@ extern "C" int abs_linear(const void* x, long long ldx, const void* w, long long
   if ((rc = check_matrix("y", y, rows, n_out, ldy, esz)) != ABS_OK) return rc;
   if (residual && (rc = check_matrix("residual", residual, rows, n_out, ldr, esz)) != ABS_OK) return rc;
   if (pre && (rc = check_matrix("pre", pre, rows, n_out, ldp, esz)) != ABS_OK) return rc;
+  if ((rc = check_vector("bias", bias, esz)) != ABS_OK) return rc;
+  if (rows == 1) { ldx = n_in; ldr = ldy = ldp = n_out; }      // (a single row has no pitch)
+  if (n_in == 1) ldw = n_out;
   const Span sx = span(x, rows, n_in, ldx, esz), sw = span(w, n_in, n_out, ldw, esz), sb = span(bias, bias ? 1 : 0, n_out, n_out, esz);
   const Span sr = span(residual, residual ? rows : 0, n_out, ldr, esz), sy = span(y, rows, n_out, ldy, esz), sp = span(pre, pre ? rows : 0, n_out, ldp, esz);
   if (overlap(sy, sx) || overlap(sy, sw) || overlap(sy, sb)) return fail(ABS_EINVAL, "y overlaps an operand");
@@ -583,7 +594,7 @@ extern "C" int abs_linear(const void* x, long long ldx, const void* w, long long
   const bool pack_x = !tma_able(x, rows, ldx), pack_w = !tma_able(w, n_in, ldw);
   if (!pack_x && few_outputs_size(rows, n_in, n_out)) return few_outputs(sa, sms, s);
   const FwdPlan f = fwd_plan(rows, n_in, n_out, dtype, pack_x, pack_w);
-  if ((rc = check_scratch(scratch, scratch_bytes, f.total)) != ABS_OK) return rc;
+  if ((rc = check_scratch(scratch, scratch_bytes, f.total, {sx, sw, sb, sr, sy, sp})) != ABS_OK) return rc;
   char* sc = (char*)scratch;
   Operand a = {x, rows, n_in, tma_pitch(rows, n_in, ldx)}, b = {w, n_in, n_out, tma_pitch(n_in, n_out, ldw)};
   if (pack_x) {
@@ -607,6 +618,7 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
   const size_t esz = dtype == ABS_FP32 ? 4 : 2;
   cudaStream_t s = (cudaStream_t)stream;
   if (dw && (rc = check_matrix("dw", dw, n_in, n_out, lddw, esz)) != ABS_OK) return rc;
+  if ((rc = check_vector("db", db, esz)) != ABS_OK) return rc;
   if (rows == 0) {
     cudaError_t e = cudaSuccess;
     if (dw) e = cudaMemset2DAsync(dw, (size_t)lddw * esz, 0, (size_t)n_out * esz, (size_t)n_in, s);
@@ -618,6 +630,8 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
   if (dx && (rc = check_matrix("w", w, n_in, n_out, ldw, esz)) != ABS_OK) return rc;
   if (dx && (rc = check_matrix("dx", dx, rows, n_in, lddx, esz)) != ABS_OK) return rc;
   if (act != ABS_ACT_NONE && (rc = check_matrix("pre", pre, rows, n_out, ldp, esz)) != ABS_OK) return rc;
+  if (rows == 1) { lddy = ldp = n_out; ldx = lddx = n_in; }
+  if (n_in == 1) ldw = lddw = n_out;
   const Span ins[4] = {span(dy, rows, n_out, lddy, esz), span(x, x ? rows : 0, n_in, ldx, esz), span(w, w ? n_in : 0, n_out, ldw, esz),
                        span(pre, act != ABS_ACT_NONE ? rows : 0, n_out, ldp, esz)};
   const Span outs[3] = {span(dx, dx ? rows : 0, n_in, lddx, esz), span(dw, dw ? n_in : 0, n_out, lddw, esz), span(db, db ? 1 : 0, n_out, n_out, esz)};
@@ -631,7 +645,7 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
   const bool need_dz = act != ABS_ACT_NONE || (bf16 && (dx || dw) && !tma_able(dy, rows, lddy));
   const bool pack_x = bf16 && dw && !tma_able(x, rows, ldx), pack_w = bf16 && dx && !tma_able(w, n_in, ldw);
   const GradPlan g = grad_plan(rows, n_in, n_out, dtype, need_dz, pack_x, pack_w);
-  if ((rc = check_scratch(scratch, scratch_bytes, g.total)) != ABS_OK) return rc;
+  if ((rc = check_scratch(scratch, scratch_bytes, g.total, {ins[0], ins[1], ins[2], ins[3], outs[0], outs[1], outs[2]})) != ABS_OK) return rc;
   int device, sms;
   if ((rc = current_device(&device, &sms)) != ABS_OK) return rc;
   char* sc = (char*)scratch;
@@ -693,6 +707,33 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
     if ((rc = tc_product(ox, 1, od, 1, n_in, n_out, rows, r, split, sms, device, s)) != ABS_OK) return rc;
   }
   return ABS_OK;
+}
+
+// One warp waits for an arrival that never comes, as the kernels of these operations wait, and reports it as they do.
+namespace {
+__global__ void op_wait_selftest_kernel(int* status, unsigned long long limit_ns) {
+  __shared__ uint64_t bar;
+  __shared__ int gave_up;
+  grid_dependency_sync();
+  if (threadIdx.x == 0) {
+    tc::mbar_init(&bar, 1);
+    gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  if (threadIdx.x == 0 && !tc::mbar_wait(&bar, 0u, &gave_up, limit_ns)) *status = 1;
+}
+}  // namespace
+
+extern "C" int abs_op_selftest_wait_timeout(int limit_us, void* stream) {
+  if (limit_us < 1 || limit_us > 1000000) return fail(ABS_EINVAL, "limit_us %d outside [1, 1000000]", limit_us);
+  int device, sms;
+  const int rc = current_device(&device, &sms);
+  if (rc != ABS_OK) return rc;
+  int* word = status_word(device);
+  if (!word) return fail(ABS_ECUDA, "cudaGetSymbolAddress(status) failed");
+  const cudaError_t e = launch(op_wait_selftest_kernel, dim3(1), 32, 0, 1, (cudaStream_t)stream, word, 1000ull * (unsigned long long)limit_us);
+  return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }
 
 extern "C" int abs_op_status(void* stream) {

@@ -137,6 +137,64 @@ def test_linear_sizes(M, K, N, bf16):
     linear_case(M, K, N, bf16, gpu.ACT_SILU, True, True, seed=M + K + N + 1)
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("M,K,N", [
+    (2, 1030, 88), (3, 1030, 88), (4, 1030, 88), (5, 1024, 88), (8, 2500, 24), (9, 2500, 24), (1, 4096, 4096), (2, 100, 6000),    # a few rows
+    (255, 256, 10), (256, 256, 10), (257, 8, 16), (400, 40, 1), (1000, 256, 16), (1000, 264, 16), (300, 512, 9), (300, 520, 9), (4000, 64, 17)])
+def test_linear_around_the_borders_of_its_kernels(M, K, N, bf16):
+    linear_case(M, K, N, bf16, gpu.ACT_GELU, True, True, seed=M + K)
+    linear_case(M, K, N, bf16, gpu.ACT_NONE, False, False, bias=False, pad=8, offset=8, seed=M + K)
+    linear_case(M, K, N, bf16, gpu.ACT_RELU, True, False, pad=1, offset=0, seed=M + K)
+
+
+@pytest.mark.parametrize("M,K,N", [(130, 5000, 136), (1, 3000, 200), (520, 100, 1032), (1100, 700, 520), (40, 33, 4100)])
+def test_linear_fp32_shared_sums(M, K, N):
+    """Sums shared by two to eight CTAs of a cluster, both tile sizes, ragged ends."""
+    linear_case(M, K, N, False, gpu.ACT_SILU, True, True, seed=K)
+    grad_case(M, K, N, False, gpu.ACT_SILU, seed=K)
+    grad_case(M, K, N, False, gpu.ACT_NONE, seed=K, want=(False, True, False))
+    grad_case(M, K, N, False, gpu.ACT_NONE, seed=K, want=(True, False, True))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_far_from_zero(act, bf16):
+    """z of both signs up to 1e30 through the forward and the backward pass, in the layer and in group norm: values and slopes of the definitions
+    (SiLU below z = -41 is zero to 4e-17, its slope too)."""
+    torch = _torch()
+    d, u = dt(bf16), half_step(bf16)
+    z = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 0.5, -0.5, 3.0, -3.0, 9.0, -9.0, 20.0, -20.0, 41.0, -41.0, 60.0, -60.0, 88.0, -88.0, 200.0, -200.0,
+                      1e4, -1e4, 1e15, -1e15, 1e30, -1e30], device="cuda").to(d)
+    n = z.numel()
+    want = act64(z.double(), act)
+    slope = torch.nan_to_num(slope64(z.double(), act), nan=0.0)
+    tol = u * want.abs() + 1e-6 * torch.clamp(z.double().abs(), max=10.0) + 1e-37
+    for rows in (1, 40, 300):
+        y = torch.empty(rows, n, device="cuda", dtype=d)
+        gpu.linear(torch.zeros(rows, 16, device="cuda", dtype=d), torch.zeros(16, n, device="cuda", dtype=d), z, None, y, act)
+        within(y, want.expand(rows, n), tol)
+        dy, x = torch.ones(rows, n, device="cuda", dtype=d), torch.zeros(rows, 16, device="cuda", dtype=d)
+        x[0, 0] = 1.0
+        db, dw = torch.empty(n, device="cuda", dtype=d), torch.empty(16, n, device="cuda", dtype=d)
+        gpu.linear_grad(dy, x, torch.zeros(16, n, device="cuda", dtype=d), z.expand(rows, n).contiguous(), None, dw, db, act)
+        within(dw[0], slope, u * slope.abs() + 2e-6)
+        within(db, rows * slope, 2 * u * rows * slope.abs() + 2e-6 * rows)
+    # group norm of constant maps: u = b
+    for P in (4, 300000):
+        b = torch.nn.functional.pad(z, (0, 32 - n))
+        y = torch.empty(1, P, 32, device="cuda", dtype=d)
+        x = torch.full((1, P, 32), 2.0, device="cuda", dtype=d)
+        mean, rstd = torch.empty(1, 2, device="cuda"), torch.empty(1, 2, device="cuda")
+        gpu.group_norm(x, 2, None, b, y, mean, rstd, 1.0, act)
+        within(y[0, 0, :n], want, tol)
+        assert bool((y[0] == y[0, 0]).all())
+        dy = torch.full((1, P, 32), 1.0 / P, device="cuda", dtype=d)
+        db = torch.empty(32, device="cuda", dtype=d)
+        gpu.group_norm_grad(dy, x, 2, None, b, mean, rstd, None, None, db, act)
+        total = float(dy.double()[0, :, 0].sum()) * slope
+        within(db[:n], total, 2 * u * total.abs() + 4e-6)
+
+
 @pytest.mark.parametrize("M,K,N", [(2300, 1000, 4096), (4224, 328, 2568), (9000, 512, 1025)])
 def test_linear_of_many_tiles(M, K, N):
     linear_case(M, K, N, True, gpu.ACT_GELU, True, True, seed=M)
@@ -310,7 +368,7 @@ def keep_mask(rows, cols, p, seed, call):
 @pytest.mark.parametrize("rows,cols,p,pad,offset", [
     (1, 1, 0.5, 0, 0), (1, 7, 0.3, 0, 0), (3, 8, 0.5, 0, 0), (5, 9, 0.5, 7, 0), (128, 256, 0.1, 0, 0), (33, 1000, 0.9, 0, 0), (200, 10, 0.5, 0, 1),
     (64, 257, 0.25, 3, 5), (1, 100003, 0.5, 0, 0), (1000, 1, 0.5, 0, 0), (7, 512, 0.999999, 0, 0), (4, 64, 0.0, 8, 8), (4, 64, 1.0, 8, 0),
-    (300, 2056, 1.0 / 65536, 0, 0)])
+    (300, 2056, 1.0 / 65536, 0, 0), (2500, 1024, 0.2, 0, 0), (2600, 1003, 0.2, 0, 0), (2600, 1000, 0.2, 1, 1)])
 def test_dropout(rows, cols, p, pad, offset, residual, bf16):
     torch = _torch()
     d, u = dt(bf16), half_step(bf16)
@@ -457,7 +515,8 @@ def norm_case(N, P, C, G, bf16, act, affine=True, pad_p=0, pad_s=0, offset=0, se
 NORM_SIZES = [
     (1, 1, 1, 1), (2, 1, 6, 3), (3, 49, 7, 7), (5, 13, 64, 64), (4, 196, 6, 2), (20, 784, 6, 3), (3, 100, 16, 1), (2, 1024, 64, 8), (2, 255, 320, 32),
     (7, 81, 84, 7), (2, 4096, 32, 4), (1, 20000, 8, 2), (1, 9000, 96, 3), (3, 16, 1000, 10), (2, 5, 4099, 1), (2, 30, 8200, 2), (1, 70000, 20, 4),
-    (64, 64, 128, 32), (2, 3000, 512, 4), (1, 300000, 16, 2), (3000, 2, 8, 2), (1, 500, 8208, 3)]
+    (64, 64, 128, 32), (2, 3000, 512, 4), (1, 300000, 16, 2), (3000, 2, 8, 2), (1, 500, 8208, 3), (50, 1000, 64, 4), (60, 1000, 120, 12), (40, 1100, 77, 7),
+    (700, 300, 30, 3), (1300, 100, 40, 1), (5, 130, 4104, 2)]
 
 
 @pytest.mark.parametrize("bf16", [False, True])
@@ -499,6 +558,22 @@ def test_group_norm_of_constant_groups(bf16):
     gpu.group_norm(x, 4, None, b, y, mean, rstd, 1e-4)
     assert torch.equal(y, b.expand(2, 9, 16)) and torch.equal(mean, torch.full_like(mean, 3.0))
     within(rstd, torch.full_like(rstd, 100.0).double(), 100 * 2.0 ** -22)
+
+
+@pytest.mark.parametrize("P", [3, 40, 100000])
+def test_group_norm_of_huge_and_tiny_values(P):
+    """Constant maps of 1e30 have no variance (threads without rows must not bring 0 times infinity into it); values of 1e-30 vanish beside eps."""
+    torch = _torch()
+    for bf16 in (False, True):
+        x = torch.full((2, P, 24), 1e30, device="cuda", dtype=dt(bf16))
+        x[1] = 1e-30
+        y = torch.empty_like(x)
+        mean, rstd = torch.empty(2, 3, device="cuda"), torch.empty(2, 3, device="cuda")
+        gpu.group_norm(x, 3, None, torch.full((24,), 0.5, device="cuda", dtype=dt(bf16)), y, mean, rstd, 1.0)
+        # (the mean of 1e30 is off by roundings; what is left of x - mean over sqrt(eps) is of their size)
+        assert bool(torch.isfinite(y).all()) and bool(torch.isfinite(mean).all()) and bool(torch.isfinite(rstd).all())
+        assert float((mean[0] / float(x[0, 0, 0].float()) - 1).abs().max()) <= (chain(P * 8) + 4) * 2.0 ** -24
+        within(y[1], torch.full_like(y[1], 0.5).double(), half_step(bf16))
 
 
 @pytest.mark.parametrize("bf16", [False, True])
@@ -758,6 +833,35 @@ def test_scratch_allocated_by_the_call_on_another_stream():
         torch.cuda.synchronize()
         outs.append((dx, dw, db))
     assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def test_a_wait_that_runs_out_is_reported_once():
+    torch = _torch()
+    gpu.op_status()
+    assert gpu.lib().abs_op_selftest_wait_timeout(1000, torch.cuda.current_stream().cuda_stream) == gpu.OK
+    with pytest.raises(gpu.AbsError) as e:
+        gpu.op_status()
+    assert e.value.code == gpu.ETIMEOUT
+    gpu.op_status()
+    test_linear_adds_to_the_residual_in_place(True)               # (the operations go on working)
+    gpu.op_status()
+
+
+def test_column_ranges_of_one_buffer():
+    """Operands and results that are column ranges of one matrix do not overlap."""
+    torch = _torch()
+    for bf16 in (False, True):
+        d = dt(bf16)
+        buf = randn(gen(8), 300, 64 + 32 + 32 + 8, dtype=d)
+        before = buf.clone()
+        w = randn(gen(9), 64, 32, dtype=d)
+        gpu.linear(buf[:, :64], w, None, buf[:, 64:96], buf[:, 96:128])
+        want = before[:, :64].double() @ w.double() + before[:, 64:96].double()
+        tol = half_step(bf16) * want.abs() + 70 * E23 * (before[:, :64].double().abs() @ w.double().abs() + before[:, 64:96].double().abs())
+        within(buf[:, 96:128], want, tol)
+        assert torch.equal(buf[:, :96], before[:, :96]) and torch.equal(buf[:, 128:], before[:, 128:])
+        with pytest.raises(gpu.AbsError):
+            gpu.linear(buf[:, :64], w, None, None, buf[:, 60:92])
 
 
 def test_layer_operations_refuse_wrong_tensors():

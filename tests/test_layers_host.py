@@ -26,7 +26,7 @@ def linear(x=A, ldx=8, w=2 * A, ldw=16, bias=0, res=0, ldr=0, y=3 * A, ldy=16, p
     (dict(rows=-1), gpu.EINVAL, "rows"), (dict(rows=1 << 31), gpu.EINVAL, "rows"), (dict(n_in=0), gpu.EINVAL, "n_in"),
     (dict(n_out=(1 << 20) + 1), gpu.EINVAL, "n_out"), (dict(x=0), gpu.EINVAL, "x is null"), (dict(w=0), gpu.EINVAL, "w is null"),
     (dict(y=0), gpu.EINVAL, "y is null"), (dict(ldx=7), gpu.EINVAL, "x: row pitch"), (dict(ldw=15), gpu.EINVAL, "w: row pitch"),
-    (dict(ldy=0), gpu.EINVAL, "y: row pitch"), (dict(x=A + 2), gpu.EINVAL, "aligned"), (dict(y=A), gpu.EINVAL, "y overlaps"),
+    (dict(ldy=0), gpu.EINVAL, "y: row pitch"), (dict(bias=4 * A + 1), gpu.EINVAL, "bias"), (dict(x=A + 2), gpu.EINVAL, "aligned"), (dict(y=A), gpu.EINVAL, "y overlaps"),
     (dict(y=2 * A + 4), gpu.EINVAL, "y overlaps"), (dict(bias=3 * A + 64), gpu.EINVAL, "y overlaps"),
     (dict(pre=3 * A, ldp=16), gpu.EINVAL, "pre overlaps"), (dict(res=3 * A + 64, ldr=16), gpu.EINVAL, "residual"),
     (dict(res=3 * A, ldr=32), gpu.EINVAL, "residual"),
@@ -51,7 +51,8 @@ def linear_grad(dy=A, lddy=16, x=2 * A, ldx=8, w=3 * A, ldw=16, pre=4 * A, ldp=1
     (dict(w=0), gpu.EINVAL, "w is null"), (dict(lddx=7), gpu.EINVAL, "dx: row pitch"), (dict(lddw=8), gpu.EINVAL, "dw: row pitch"),
     (dict(ldp=15), gpu.EINVAL, "pre: row pitch"), (dict(dx=A), gpu.EINVAL, "overlaps an operand"), (dict(dw=3 * A), gpu.EINVAL, "overlaps an operand"),
     (dict(db=6 * A), gpu.EINVAL, "two gradients"), (dict(sz=0), gpu.ENOSPACE, "scratch holds 0"), (dict(scratch=0), gpu.EINVAL, "scratch"),
-    (dict(scratch=8 * A + 16), gpu.EINVAL, "scratch"), (dict(act=7), gpu.EUNSUPPORTED, "activation"),
+    (dict(scratch=8 * A + 16), gpu.EINVAL, "scratch"), (dict(scratch=A), gpu.EINVAL, "scratch overlaps"), (dict(db=7 * A + 2), gpu.EINVAL, "db"),
+    (dict(act=7), gpu.EUNSUPPORTED, "activation"),
 ])
 def test_linear_grad_refuses(kw, code, text):
     assert linear_grad(**kw) == code
@@ -107,6 +108,25 @@ def norm(x=A, xs=160, xp=16, y=2 * A, ys=160, yp=16, mean=0, rstd=0, n=4, pos=10
 def test_group_norm_refuses(kw, code, text):
     assert norm(**kw) == code
     assert text in gpu.last_error()
+
+
+def test_group_norm_refuses_overlapping_vectors():
+    f = gpu.lib().abs_group_norm
+    for w, b, mean, rstd, text in ((2 * A, None, None, None, "y overlaps w or b"), (3 * A + 2, None, None, None, "w is not aligned"),
+                                   (None, None, 4 * A, 4 * A + 4, "mean overlaps rstd"), (None, None, A, 4 * A, "mean or rstd overlaps"),
+                                   (None, None, 4 * A + 2, 5 * A, "mean is not aligned")):
+        assert f(A, 160, 16, w, b, 2 * A, 160, 16, mean, rstd, 4, 10, 16, 4, 1e-5, 0, 0, None, 0, None) == gpu.EINVAL
+        assert text in gpu.last_error()
+    g = gpu.lib().abs_group_norm_grad
+    for dw, db, text in ((A, None, "a gradient overlaps"), (6 * A, 6 * A + 4, "two gradients"), (3 * A, None, "a gradient overlaps"),
+                         (5 * A, None, "two gradients"), (6 * A + 1, None, "dw is not aligned")):
+        assert g(A, 160, 16, 2 * A, 160, 16, None, None, 3 * A, 4 * A, 5 * A, 160, 16, dw, db, 4, 10, 16, 4, 0, 0, None, 0, None) == gpu.EINVAL
+        assert text in gpu.last_error()
+
+
+def test_wait_selftest_limits():
+    assert gpu.lib().abs_op_selftest_wait_timeout(0, None) == gpu.EINVAL
+    assert gpu.lib().abs_op_selftest_wait_timeout(1000001, None) == gpu.EINVAL
 
 
 def norm_grad(dy=A, ds=160, dp=16, x=2 * A, xs=160, xp=16, mean=3 * A, rstd=4 * A, dx=5 * A, dxs=160, dxp=16, n=4, pos=10, ch=16, groups=4, act=0,
