@@ -560,6 +560,13 @@ def test_group_norm_of_constant_groups(bf16):
     within(rstd, torch.full_like(rstd, 100.0).double(), 100 * 2.0 ** -22)
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("N,P,C,G", [(1, 300000, 16, 2), (700, 300, 30, 3), (2, 30, 8200, 2)])
+def test_group_norm_in_place_of_large_maps(N, P, C, G, bf16):
+    norm_case(N, P, C, G, bf16, gpu.ACT_SILU, seed=N, in_place=True)
+    norm_grad_case(N, P, C, G, bf16, gpu.ACT_SILU, seed=N, in_place=True)
+
+
 @pytest.mark.parametrize("P", [3, 40, 100000])
 def test_group_norm_of_huge_and_tiny_values(P):
     """Constant maps of 1e30 have no variance (threads without rows must not bring 0 times infinity into it); values of 1e-30 vanish beside eps."""
@@ -833,6 +840,34 @@ def test_scratch_allocated_by_the_call_on_another_stream():
         torch.cuda.synchronize()
         outs.append((dx, dw, db))
     assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_a_trained_model_evaluated_on_its_data(bf16):
+    """get_params of a run, layer by layer through `linear` over the whole dataset, against the same in 64 bits."""
+    torch = _torch()
+    from paper_2301_08895_b200 import inputs
+    cfg = inputs.config(3).scaled(n_samples=4096, dtype=inputs.BF16 if bf16 else inputs.FP32)
+    X, y, _ = inputs.make_data(cfg)
+    Xd = torch.from_numpy(X.view(np.int16)).cuda().view(torch.bfloat16) if bf16 else torch.from_numpy(X).cuda()
+    ctx = gpu.context_from_config(cfg, Xd, torch.from_numpy(y).cuda(), inputs.make_w0(cfg), max_rounds=4)
+    ctx.run_rounds(4)
+    params = ctx.get_params()
+    ctx.close()
+    d, off, h, h64 = dt(bf16), 0, Xd, Xd.double()
+    for l in range(2):
+        i, o = cfg.dims[l], cfg.dims[l + 1]
+        w = torch.from_numpy(params[off:off + i * o].reshape(i, o)).cuda().to(d)
+        b = torch.from_numpy(params[off + i * o:off + i * o + o]).cuda().to(d)
+        off += i * o + o
+        act = gpu.ACT_RELU if l == 0 else gpu.ACT_NONE
+        out = torch.empty(h.shape[0], o, device="cuda", dtype=d)
+        gpu.linear(h, w, b, None, out, act)
+        h64 = act64(h64 @ w.double() + b.double(), act)
+        h = out
+    # two stored layers: each rounded by half a step, the first one's rounding goes through the second
+    assert float((h.double() - h64).norm()) <= 3 * (half_step(bf16) + 800 * E23) * float(h64.norm())
+    assert off == params.size
 
 
 def test_a_wait_that_runs_out_is_reported_once():
