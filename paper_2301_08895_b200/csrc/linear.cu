@@ -155,12 +155,12 @@ __global__ void __launch_bounds__(256) column_kernel(const float* part, int chun
 struct FinishArgs {
   const float* part;
   int splits, I, J, Jp;                  // Jp: pitch of a partial row
-  const __nv_bfloat16* bias; const __nv_bfloat16* res; __nv_bfloat16* out; __nv_bfloat16* pre;
+  const void* bias; const void* res; void* out; void* pre;
   long long ldr, ldo, ldp;
   Divisor quads;                         // groups of four columns per row
   uint32_t n;                            // groups
 };
-template <int ACT>
+template <typename T, int ACT>
 __global__ void __launch_bounds__(256) finish_kernel(FinishArgs a) {
   grid_dependency_sync();
   for (uint32_t q = blockIdx.x * 256u + threadIdx.x; q < a.n; q += gridDim.x * 256u) {
@@ -178,15 +178,15 @@ __global__ void __launch_bounds__(256) finish_kernel(FinishArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {                        // (all loads in front of the stores, which may alias them)
       const bool in = (int)j + e < a.J;
-      bias[e] = a.bias && in ? __bfloat162float(a.bias[j + e]) : 0.f;
-      res[e] = a.res && in ? __bfloat162float(a.res[(long long)i * a.ldr + j + e]) : 0.f;
+      bias[e] = a.bias && in ? ldf((const T*)a.bias, j + e) : 0.f;
+      res[e] = a.res && in ? ldf((const T*)a.res, (long long)i * a.ldr + j + e) : 0.f;
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if ((int)j + e >= a.J) break;
       const float v = z[e] + bias[e];
-      if (a.pre) a.pre[(long long)i * a.ldp + j + e] = __float2bfloat16_rn(v);
-      a.out[(long long)i * a.ldo + j + e] = __float2bfloat16_rn(act_value<ACT>(v) + res[e]);
+      if (a.pre) stf((T*)a.pre, (long long)i * a.ldp + j + e, v);
+      stf((T*)a.out, (long long)i * a.ldo + j + e, act_value<ACT>(v) + res[e]);
     }
   }
 }
@@ -215,13 +215,26 @@ SlopeFn slope_fn(int dtype, bool vec, int act) {
   if (dtype == ABS_FP32) return vec ? ACT_FN(SlopeFn, slope_kernel, act, float, 4) : ACT_FN(SlopeFn, slope_kernel, act, float, 1);
   return vec ? ACT_FN(SlopeFn, slope_kernel, act, __nv_bfloat16, 8) : ACT_FN(SlopeFn, slope_kernel, act, __nv_bfloat16, 1);
 }
-typedef void (*FinishFn)(FinishArgs);
-FinishFn finish_fn(int act) {
-  return act == ABS_ACT_RELU ? (FinishFn)finish_kernel<ABS_ACT_RELU> : act == ABS_ACT_GELU ? (FinishFn)finish_kernel<ABS_ACT_GELU>
-         : act == ABS_ACT_SILU ? (FinishFn)finish_kernel<ABS_ACT_SILU> : (FinishFn)finish_kernel<ABS_ACT_NONE>;
-}
-
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
+
+struct Operand { const void* p; long long rows, cols, ld; };     // a stored matrix that TMA can address
+struct Result {
+  const void* bias; const void* res; long long ldr;
+  void* out; long long ldo; void* pre; long long ldp;
+  int act;
+};
+
+typedef void (*FinishFn)(FinishArgs);
+template <typename T> cudaError_t finish(const float* part, int splits, int I, int J, const Result& r, int sms, cudaStream_t s) {
+  FinishArgs f = {};
+  f.part = part; f.splits = splits; f.I = I; f.J = J; f.Jp = (J + 3) / 4 * 4;
+  f.bias = r.bias; f.res = r.res; f.out = r.out; f.pre = r.pre;
+  f.ldr = r.ldr; f.ldo = r.ldo; f.ldp = r.ldp;
+  f.quads = Divisor((uint32_t)(f.Jp / 4));
+  f.n = (uint32_t)((size_t)I * (f.Jp / 4));              // (partial results hold at most 2^26 floats)
+  const unsigned blocks = (f.n + 255) / 256;
+  return launch(ACT_FN(FinishFn, finish_kernel, r.act, T), dim3(blocks < 8u * sms ? blocks : 8u * sms), 256, 0, 1, s, f);
+}
 
 // ------------------------------------------------------------------ tensor-core products (bf16)
 
@@ -297,13 +310,6 @@ bool tma_able(const void* p, long long rows, long long ld) { return (uintptr_t)p
 long long tma_pitch(long long rows, long long cols, long long ld) { return rows == 1 ? (cols + 7) / 8 * 8 : ld; }
 size_t pack_bytes(long long rows, long long cols) { return round256((size_t)rows * ((cols + 7) / 8 * 8) * 2); }
 
-struct Operand { const void* p; long long rows, cols, ld; };     // a stored matrix that TMA can address
-struct Result {
-  const void* bias; const void* res; long long ldr;
-  void* out; long long ldo; void* pre; long long ldp;
-  int act;
-};
-
 template <int BN, int CG>
 cudaError_t launch_dense(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const CUtensorMap& z, const dense::Args& p, int sms, int device,
                          cudaStream_t s) {
@@ -364,16 +370,7 @@ int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, in
   if (!ok) return fail(ABS_ECUDA, "cuTensorMapEncodeTiled failed");
   cudaError_t e = pl.cg == 2 ? (pl.bn == 256 ? launch_dense<256, 2>(ma, mb, mo, mz, p, sms, device, s) : launch_dense<128, 2>(ma, mb, mo, mz, p, sms, device, s)) : pl.bn == 256 ? launch_dense<256, 1>(ma, mb, mo, mz, p, sms, device, s)
                   : pl.bn == 128 ? launch_dense<128, 1>(ma, mb, mo, mz, p, sms, device, s) : launch_dense<64, 1>(ma, mb, mo, mz, p, sms, device, s);
-  if (e == cudaSuccess && pl.splits > 1) {
-    FinishArgs f = {};
-    f.part = part; f.splits = pl.splits; f.I = I; f.J = J; f.Jp = Jp;
-    f.bias = (const __nv_bfloat16*)r.bias; f.res = (const __nv_bfloat16*)r.res; f.out = (__nv_bfloat16*)r.out; f.pre = (__nv_bfloat16*)r.pre;
-    f.ldr = r.ldr; f.ldo = r.ldo; f.ldp = r.ldp;
-    f.quads = Divisor((uint32_t)(Jp / 4));
-    f.n = (uint32_t)((size_t)I * (Jp / 4));              // (partial results hold at most 2^26 floats)
-    const unsigned blocks = (f.n + 255) / 256;
-    e = launch(finish_fn(r.act), dim3(blocks < 8u * sms ? blocks : 8u * sms), 256, 0, 1, s, f);
-  }
+  if (e == cudaSuccess && pl.splits > 1) e = finish<__nv_bfloat16>(part, pl.splits, I, J, r, sms, s);
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }
 
@@ -387,25 +384,32 @@ int pack(const void* src, long long rows, long long cols, long long ld, void* ds
 
 // ------------------------------------------------------------------ fp32 products
 
-struct FmaPlan { int bm, Q, kb_per; };
-// 64 x 64 or 128 x 128 tiles, and how many CTAs share a tile's sum.  A block of 32 k takes a CTA that is alone on its SM 0.95 or 3.3
-// us, two of them together 1.7 or 5.8 us (4096^3: 54 TFLOP/s); joining CTAs costs about a microsecond.  CLUSTERS: clusters of q CTAs,
-// two per SM, that the GPU runs at a time (one more than that takes a second round: 72 clusters of four 150 us, pairs 126).  Rows that
-// do not start on 16 bytes (lines = false) cost the small tile another microsecond for two CTAs' block: their copies touch a line more.
-FmaPlan plan_fma(long long I, int J, int K, bool lines) {
+struct FmaPlan { int bm, Q, splits, kb_per; size_t part_bytes; };
+// 64 x 64 or 128 x 128 tiles, how many CTAs of a cluster share a tile's sum, and into how many parts that go through scratch it is cut
+// besides.  A block of 32 k takes a CTA that is alone on its SM 0.95 or 3.3 us, two of them together 1.7 or 5.8 us (4096^3: 54
+// TFLOP/s); a round of CTAs costs 3 to 5 us for filling and results, a microsecond more in clusters, parts their way through L2 and a
+// launch.  CLUSTERS: clusters of q CTAs, two per SM, that the GPU runs at a time (72 clusters of four 150 us, pairs 126).
+FmaPlan plan_fma(long long I, int J, int K) {
   static const int CLUSTERS[9] = {0, 296, 148, 93, 71, 56, 45, 37, 33};
   FmaPlan best = {};
   double least = 1e300;
   const int n_kb = (K + fp32::BK - 1) / fp32::BK;
+  const long long Jp = (J + 3) / 4 * 4;
   for (int bm : {64, 128}) {
     const long long tiles = (I + bm - 1) / bm * ((J + bm - 1) / bm);
-    const double one = bm == 64 ? (lines ? 0.95 : 1.4) : 3.3, two = bm == 64 ? (lines ? 1.7 : 2.8) : 5.8;
-    for (int q = 1; q <= 8 && q <= n_kb; ++q) {
-      const int per = (n_kb + q - 1) / q;
-      if ((q - 1) * per >= n_kb) continue;
-      const long long full = tiles / CLUSTERS[q], rest = tiles - full * CLUSTERS[q];
-      const double t = ((double)full * two + (rest * q > PLAN_SMS - 12 ? two : rest > 0 ? one : 0.0)) * per + (bm == 64 ? 3.0 : 5.0) + (q > 1 ? 1.0 : 0.0);
-      if (t < least) { least = t; best = FmaPlan{bm, q, per}; }
+    const double one = bm == 64 ? 0.95 : 3.3, two = bm == 64 ? 1.7 : 5.8;
+    for (int split = 1; split <= 64; split *= 2) {
+      const size_t bytes = split > 1 ? round256((size_t)split * (I * Jp + J) * 4) : 0;
+      if (split > 1 && (bytes > (64u << 20) || tiles * (split / 2) > 2 * PLAN_SMS)) break;
+      for (int q = 1; q <= 8; ++q) {
+        const int chunks = q * split, per = (n_kb + chunks - 1) / chunks;
+        if ((long long)(chunks - 1) * per >= n_kb) continue;     // (a part would be empty)
+        const long long n = tiles * split, full = n / CLUSTERS[q], rest = n - full * CLUSTERS[q];
+        const double around = (bm == 64 ? 3.0 : 5.0) + (q > 1 ? 1.0 : 0.0);
+        const double last = rest == 0 ? 0.0 : (rest * q > PLAN_SMS - 12 ? two : one) * per + around;
+        const double t = (double)full * (two * per + around) + last + (split > 1 ? 2.5 + (double)bytes * 2.0 / 6e6 : 0.0);
+        if (t < least) { least = t; best = FmaPlan{bm, q, split, per, bytes}; }
+      }
     }
   }
   return best;
@@ -415,7 +419,7 @@ template <int BM> FmaFn fma_fn(int act) {
   return act == ABS_ACT_RELU ? (FmaFn)fp32::fma_kernel<BM, BM, ABS_ACT_RELU> : act == ABS_ACT_GELU ? (FmaFn)fp32::fma_kernel<BM, BM, ABS_ACT_GELU>
          : act == ABS_ACT_SILU ? (FmaFn)fp32::fma_kernel<BM, BM, ABS_ACT_SILU> : (FmaFn)fp32::fma_kernel<BM, BM, ABS_ACT_NONE>;
 }
-int fma_product(fp32::Args p, long long I, int J, int K, int act, int device, cudaStream_t s) {
+int fma_product(fp32::Args p, const FmaPlan& pl, long long I, int J, int K, int act, float* part, int sms, int device, cudaStream_t s) {
   static std::atomic<uint64_t> ready;
   cudaError_t e = cudaSuccess;
   if (!(ready.load(std::memory_order_acquire) >> device & 1)) {
@@ -428,18 +432,34 @@ int fma_product(fp32::Args p, long long I, int J, int K, int act, int device, cu
   }
   for (long long pitch : {p.a_i, p.a_k, p.b_k, p.b_j})
     if (pitch > (1ll << 24)) return fail(ABS_EUNSUPPORTED, "fp32: row pitch %lld above 2^24", pitch);
-  const bool lines = ((uintptr_t)p.a | (uintptr_t)p.b) % 16 == 0 && (p.a_i == 1 ? p.a_k : p.a_i) % 4 == 0 && (p.b_j == 1 ? p.b_k : p.b_j) % 4 == 0;
-  const FmaPlan pl = plan_fma(I, J, K, lines);
   p.I = (int)I; p.J = J; p.K = K;
   p.n_kb = (K + fp32::BK - 1) / fp32::BK;
   p.n_jt = (J + pl.bm - 1) / pl.bm;
   p.Q = pl.Q; p.kb_per = pl.kb_per;
   p.by_Q = Divisor((uint32_t)pl.Q);
   p.by_njt = Divisor((uint32_t)p.n_jt);
-  const long long ctas = (I + pl.bm - 1) / pl.bm * p.n_jt * pl.Q;
+  const long long tiles = (I + pl.bm - 1) / pl.bm * p.n_jt, ctas = tiles * pl.splits * pl.Q;
+  const fp32::Args whole = p;
+  if (pl.splits > 1) {
+    p.bias = p.res = nullptr;
+    p.pre = nullptr;
+    p.ldo = (J + 3) / 4 * 4;
+    p.out = part;
+    p.out_step = I * p.ldo;
+    p.col_step = J;
+    if (p.colsum) p.colsum = part + pl.splits * p.out_step;
+  }
+  p.by_tiles = Divisor((uint32_t)(tiles < 0x7fffffff ? tiles : 1));
   if (ctas > 0x7fffffff) return fail(ABS_EUNSUPPORTED, "%lld tiles in one product", ctas);
-  e = pl.bm == 64 ? launch(fma_fn<64>(act), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<64, 64>::SMEM, pl.Q, s, p)
-                  : launch(fma_fn<128>(act), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<128, 128>::SMEM, pl.Q, s, p);
+  const int in_kernel = pl.splits > 1 ? ABS_ACT_NONE : act;
+  e = pl.bm == 64 ? launch(fma_fn<64>(in_kernel), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<64, 64>::SMEM, pl.Q, s, p)
+                  : launch(fma_fn<128>(in_kernel), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<128, 128>::SMEM, pl.Q, s, p);
+  if (e == cudaSuccess && pl.splits > 1) {
+    const Result r = {whole.bias, whole.res, whole.ldr, whole.out, whole.ldo, whole.pre, whole.ldp, act};
+    e = finish<float>(part, pl.splits, (int)I, J, r, sms, s);
+    if (e == cudaSuccess && whole.colsum)
+      e = launch(column_kernel<float>, dim3((unsigned)((J + 31) / 32)), 256, 0, 1, s, (const float*)p.colsum, pl.splits, J, (void*)whole.colsum);
+  }
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }
 
@@ -511,16 +531,20 @@ int check_matrix(const char* name, const void* p, long long rows, long long cols
 }
 
 // Scratch of a call.  need_*: the operand is copied to a pitch that TMA can address (bf16).
-struct FwdPlan { size_t x, w, part, total; };
+struct FwdPlan { size_t x, w, part, total; FmaPlan fma; };
 FwdPlan fwd_plan(long long rows, int n_in, int n_out, int dtype, bool pack_x, bool pack_w) {
   FwdPlan f = {};
-  if (dtype == ABS_FP32) return f;
+  if (dtype == ABS_FP32) {
+    f.fma = plan_fma(rows, n_out, n_in);
+    f.total = f.fma.part_bytes;
+    return f;
+  }
   f.w = pack_x ? pack_bytes(rows, n_in) : 0;
   f.part = f.w + (pack_w ? pack_bytes(n_in, n_out) : 0);
   f.total = f.part + plan_product(rows, n_out, n_in).part_bytes;
   return f;
 }
-struct GradPlan { size_t dz, sums, x, w, part, total; long long ld_dz; int chunk, chunks; };
+struct GradPlan { size_t dz, sums, x, w, part, total; long long ld_dz; int chunk, chunks; FmaPlan dx, dw; };
 GradPlan grad_plan(long long rows, int n_in, int n_out, int dtype, bool need_dz, bool pack_x, bool pack_w) {
   GradPlan g = {};
   const size_t esz = dtype == ABS_FP32 ? 4 : 2;
@@ -535,11 +559,14 @@ GradPlan grad_plan(long long rows, int n_in, int n_out, int dtype, bool need_dz,
   g.x = g.sums + round256((size_t)g.chunks * n_out * 4);
   g.w = g.x + (pack_x ? pack_bytes(rows, n_in) : 0);
   g.part = g.w + (pack_w ? pack_bytes(n_in, n_out) : 0);
-  g.total = g.part;
-  if (dtype != ABS_FP32) {
-    const size_t a = plan_product(rows, n_in, n_out).part_bytes, b = plan_product(n_in, n_out, rows).part_bytes;
-    g.total += a > b ? a : b;
+  size_t a, b;
+  if (dtype == ABS_FP32) {
+    g.dx = plan_fma(rows, n_in, n_out); g.dw = plan_fma(n_in, n_out, (int)rows);
+    a = g.dx.part_bytes; b = g.dw.part_bytes;
+  } else {
+    a = plan_product(rows, n_in, n_out).part_bytes; b = plan_product(n_in, n_out, rows).part_bytes;
   }
+  g.total = g.part + (a > b ? a : b);
   return g;
 }
 
@@ -578,23 +605,25 @@ extern "C" int abs_linear(const void* x, long long ldx, const void* w, long long
   if (overlap(sy, sx) || overlap(sy, sw) || overlap(sy, sb)) return fail(ABS_EINVAL, "y overlaps an operand");
   if (overlap(sp, sx) || overlap(sp, sw) || overlap(sp, sb) || overlap(sp, sr) || overlap(sp, sy)) return fail(ABS_EINVAL, "pre overlaps another matrix");
   if (overlap(sy, sr) && !(y == residual && ldy == ldr)) return fail(ABS_EINVAL, "y overlaps residual without being the same matrix");
+  const bool few = rows <= few_rows_limit(dtype), bf16 = dtype != ABS_FP32;
+  const bool pack_x = bf16 && !tma_able(x, rows, ldx), pack_w = bf16 && !tma_able(w, n_in, ldw);
+  const bool narrow = !few && bf16 && !pack_x && few_outputs_size(rows, n_in, n_out);
+  const FwdPlan f = few || narrow ? FwdPlan{} : fwd_plan(rows, n_in, n_out, dtype, pack_x, pack_w);
+  if ((rc = check_scratch(scratch, scratch_bytes, f.total, {sx, sw, sb, sr, sy, sp})) != ABS_OK) return rc;
   cudaStream_t s = (cudaStream_t)stream;
   int device, sms;
   if ((rc = current_device(&device, &sms)) != ABS_OK) return rc;
   const small::Args sa = {x, w, bias, residual, y, pre, ldx, ldw, ldr, ldy, ldp, rows, n_in, n_out, act};
-  if (rows <= few_rows_limit(dtype)) return few_rows(sa, dtype, s);
+  if (few) return few_rows(sa, dtype, s);
+  if (narrow) return few_outputs(sa, sms, s);
   if (dtype == ABS_FP32) {
     fp32::Args p = {};
     p.a = (const float*)x; p.a_i = ldx; p.a_k = 1;
     p.b = (const float*)w; p.b_k = ldw; p.b_j = 1;
     p.bias = (const float*)bias; p.res = (const float*)residual; p.out = (float*)y; p.pre = (float*)pre;
     p.ldr = ldr; p.ldo = ldy; p.ldp = ldp;
-    return fma_product(p, rows, n_out, n_in, act, device, s);
+    return fma_product(p, f.fma, rows, n_out, n_in, act, (float*)scratch, sms, device, s);
   }
-  const bool pack_x = !tma_able(x, rows, ldx), pack_w = !tma_able(w, n_in, ldw);
-  if (!pack_x && few_outputs_size(rows, n_in, n_out)) return few_outputs(sa, sms, s);
-  const FwdPlan f = fwd_plan(rows, n_in, n_out, dtype, pack_x, pack_w);
-  if ((rc = check_scratch(scratch, scratch_bytes, f.total, {sx, sw, sb, sr, sy, sp})) != ABS_OK) return rc;
   char* sc = (char*)scratch;
   Operand a = {x, rows, n_in, tma_pitch(rows, n_in, ldx)}, b = {w, n_in, n_out, tma_pitch(n_in, n_out, ldw)};
   if (pack_x) {
@@ -674,7 +703,7 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
       p.a = (const float*)dz; p.a_i = lddz; p.a_k = 1;
       p.b = (const float*)w; p.b_k = 1; p.b_j = ldw;
       p.out = (float*)dx; p.ldo = lddx;
-      if ((rc = fma_product(p, rows, n_in, n_out, ABS_ACT_NONE, device, s)) != ABS_OK) return rc;
+      if ((rc = fma_product(p, g.dx, rows, n_in, n_out, ABS_ACT_NONE, (float*)(sc + g.part), sms, device, s)) != ABS_OK) return rc;
     }
     if (dw) {
       fp32::Args p = {};
@@ -682,7 +711,7 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
       p.b = (const float*)dz; p.b_k = lddz; p.b_j = 1;
       p.out = (float*)dw; p.ldo = lddw;
       p.colsum = with_dw ? (float*)db : nullptr;
-      if ((rc = fma_product(p, n_in, n_out, (int)rows, ABS_ACT_NONE, device, s)) != ABS_OK) return rc;
+      if ((rc = fma_product(p, g.dw, n_in, n_out, (int)rows, ABS_ACT_NONE, (float*)(sc + g.part), sms, device, s)) != ABS_OK) return rc;
     }
     return ABS_OK;
   }

@@ -7,7 +7,8 @@
 // loop over shared memory: 61 TFLOP/s in this form, 59 with single FMAs, 50 to 57 with pairs of even and odd k, which need no doubling.)
 // 64 x 64 tiles have four groups of 64 threads that take eight k of a block each (KG = 4), added at
 // the end; and a cluster of Q CTAs can share a tile's sum: each leaves its part in shared memory, takes 1 / Q of the tile's rows,
-// adds the parts in the order of the ranks and applies the epilogue.
+// adds the parts in the order of the ranks and applies the epilogue.  A long sum of few tiles is cut into parts besides, which a second
+// kernel adds.
 #pragma once
 #include "layerops.cuh"
 
@@ -24,7 +25,8 @@ struct Args {
   const float* bias; const float* res; float* out; float* pre;
   long long ldr, ldo, ldp;
   float* colsum;                         // sums of B's columns (null: none), by the CTAs of the first row tile
-  layer::Divisor by_Q, by_njt;
+  long long out_step; int col_step;      // part number s of a sum cut in parts goes to out + s out_step, colsum + s col_step
+  layer::Divisor by_Q, by_njt, by_tiles; // by_tiles: tiles of one part
 };
 
 template <int BM, int BN> struct Cfg {
@@ -115,12 +117,12 @@ __global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Args
   using C = Cfg<BM, BN>;
   constexpr int STAGES = C::STAGES, KG = C::KG, KPG = BK / KG, TX = BN / 8;
   extern __shared__ __align__(16) float sm[];
-  const uint32_t tile = p.by_Q.div(blockIdx.x);
-  const int rank = (int)(blockIdx.x - tile * p.by_Q.d);
+  const uint32_t work = p.by_Q.div(blockIdx.x), part = p.out_step ? p.by_tiles.div(work) : 0u, tile = work - part * p.by_tiles.d;
+  const int rank = (int)(blockIdx.x - work * p.by_Q.d);
   const uint32_t it = p.by_njt.div(tile);
   const long long i0 = (long long)it * BM;
   const int j0 = (int)(tile - it * p.by_njt.d) * BN;
-  const int kb0 = rank * p.kb_per, nkb = min(p.kb_per, p.n_kb - kb0);
+  const int kb0 = ((int)part * p.Q + rank) * p.kb_per, nkb = min(p.kb_per, p.n_kb - kb0);
   grid_dependency_sync();
 
   const int X = (int)min((long long)BM, p.I - i0), Y = min(BN, p.J - j0);
@@ -232,7 +234,7 @@ __global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Args
     const long long i = i0 + r;
     const float v = z + bias;
     if (p.pre) p.pre[i * p.ldp + j0 + c] = v;
-    p.out[i * p.ldo + j0 + c] = layer::act_value<ACT>(v) + res;
+    p.out[part * p.out_step + i * p.ldo + j0 + c] = layer::act_value<ACT>(v) + res;
   };
   constexpr int U = 4;
 #pragma unroll 1
@@ -261,7 +263,7 @@ __global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Args
   if (sums && rank == 0 && (int)threadIdx.x < Y) {
     float z = cs;
     for (int q = 1; q < p.Q; ++q) z += ld_peer(cs_sm + threadIdx.x, q);
-    p.colsum[j0 + threadIdx.x] = z;
+    p.colsum[(size_t)part * p.col_step + j0 + threadIdx.x] = z;
   }
   if (p.Q > 1) {                         // nobody leaves while a peer reads its part
     __syncwarp();

@@ -303,6 +303,48 @@ def test_linear_grad_sizes(M, K, N, bf16):
     grad_case(M, K, N, bf16, gpu.ACT_SILU, seed=M + 1)
 
 
+@pytest.mark.parametrize("pad,offset", [(0, 0), (1, 0), (8, 8)])
+@pytest.mark.parametrize("M,K,N", [(3001, 20, 17), (9001, 37, 29), (20011, 130, 70), (70, 65, 12001)])
+def test_linear_fp32_long_sums(M, K, N, pad, offset):
+    """Long sums of few tiles: parts through scratch, with and without clusters in each."""
+    linear_case(70, M, N % 500, False, gpu.ACT_GELU, True, True, pad=pad, offset=offset, seed=M)
+    linear_case(70, M, K, False, gpu.ACT_NONE, False, False, pad=pad, offset=offset, seed=M, bias=False)
+    grad_case(M, K, N, False, gpu.ACT_SILU, pad=pad, offset=offset, seed=M)
+    grad_case(M, K, N, False, gpu.ACT_NONE, pad=pad, offset=offset, seed=M, want=(False, True, True))
+    grad_case(M, K, N, False, gpu.ACT_RELU, pad=pad, offset=offset, seed=M, want=(True, False, False))
+
+
+def test_linear_fp32_parts_in_a_captured_step():
+    """The scratch of a call serves the next one on its stream: forward, gradients and forward again in one graph, replayed, give the same bits."""
+    torch = _torch()
+    g = gen(5)
+    x, w, dy = randn(g, 3001, 20), randn(g, 20, 17), randn(g, 3001, 17)
+    a, b = randn(g, 70, 3001), randn(g, 3001, 17)
+    y, dw, db, dx, again = torch.empty(70, 17, device="cuda"), torch.empty_like(w), torch.empty(17, device="cuda"), torch.empty_like(x), torch.empty(70, 17, device="cuda")
+    size = max(gpu.linear_scratch_bytes(70, 3001, 17, dtype=gpu.FP32), gpu.linear_scratch_bytes(3001, 20, 17, dtype=gpu.FP32, grad=True))
+    assert size > 0
+    scratch = torch.empty(size, dtype=torch.uint8, device="cuda")
+
+    def step():
+        gpu.linear(a, b, None, None, y, scratch=scratch)
+        gpu.linear_grad(dy, x, w, None, dx, dw, db, scratch=scratch)
+        gpu.linear(a, b, None, None, again, scratch=scratch)
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (y, dw, db, dx, again)]
+    assert torch.equal(y, again)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for t in (y, dw, db, dx, again):
+        t.fill_(float("nan"))
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    for t, v in zip((y, dw, db, dx, again), want):
+        assert torch.equal(t, v)
+
+
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("want", [(True, False, False), (False, True, False), (False, False, True), (True, True, False)])

@@ -37,6 +37,16 @@ def test_linear_refuses(kw, code, text):
     assert text in gpu.last_error()
 
 
+def test_linear_fp32_long_sum_needs_scratch():
+    need = gpu.linear_scratch_bytes(64, 4096, 64, dtype=gpu.FP32)
+    assert need >= 2 * 64 * 64 * 4
+    far = dict(rows=64, n_in=4096, ldx=4096, n_out=64, ldw=64, ldy=64, x=A, w=2 * A, y=3 * A)
+    for kw, code, text in ((dict(sz=need - 1, scratch=8 * A), gpu.ENOSPACE, "scratch holds"), (dict(sz=need), gpu.EINVAL, "scratch"),
+                           (dict(sz=need, scratch=2 * A + 256), gpu.EINVAL, "scratch overlaps")):
+        assert linear(**far, **kw) == code
+        assert text in gpu.last_error()
+
+
 def test_linear_without_rows_needs_no_matrices():
     assert linear(x=0, w=0, y=0, rows=0) == gpu.OK
 
