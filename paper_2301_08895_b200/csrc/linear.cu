@@ -159,10 +159,12 @@ struct FinishArgs {
   long long ldr, ldo, ldp;
   Divisor quads;                         // groups of four columns per row
   uint32_t n;                            // groups
+  const uint32_t* flags; int n_flags;    // no work if one of these is raised
 };
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256) finish_kernel(FinishArgs a) {
   grid_dependency_sync();
+  if (a.flags && split3::any_flag(a.flags, a.n_flags)) return;
   for (uint32_t q = blockIdx.x * 256u + threadIdx.x; q < a.n; q += gridDim.x * 256u) {
     const uint32_t i = a.quads.div(q), j = 4u * (q - i * a.quads.d);
     const float* p = a.part + (size_t)i * a.Jp + j;
@@ -225,13 +227,15 @@ struct Result {
 };
 
 typedef void (*FinishFn)(FinishArgs);
-template <typename T> cudaError_t finish(const float* part, int splits, int I, int J, const Result& r, int sms, cudaStream_t s) {
+struct Flags { uint32_t* p; int n; };
+template <typename T> cudaError_t finish(const float* part, int splits, int I, int J, const Result& r, const Flags& flags, int sms, cudaStream_t s) {
   FinishArgs f = {};
   f.part = part; f.splits = splits; f.I = I; f.J = J; f.Jp = (J + 3) / 4 * 4;
   f.bias = r.bias; f.res = r.res; f.out = r.out; f.pre = r.pre;
   f.ldr = r.ldr; f.ldo = r.ldo; f.ldp = r.ldp;
+  f.flags = flags.p; f.n_flags = flags.n;
   f.quads = Divisor((uint32_t)(f.Jp / 4));
-  f.n = (uint32_t)((size_t)I * (f.Jp / 4));              // (partial results hold at most 2^26 floats)
+  f.n = (uint32_t)((size_t)I * (f.Jp / 4));              // (partial results hold at most 2^28 floats)
   const unsigned blocks = (f.n + 255) / 256;
   return launch(ACT_FN(FinishFn, finish_kernel, r.act, T), dim3(blocks < 8u * sms ? blocks : 8u * sms), 256, 0, 1, s, f);
 }
@@ -239,13 +243,14 @@ template <typename T> cudaError_t finish(const float* part, int splits, int I, i
 // ------------------------------------------------------------------ tensor-core products (bf16)
 
 // How a product C[I][J] = sum over K terms is cut up.
-struct Plan { int bn, cg, splits, kb_per; size_t part_bytes; };
+struct Plan { int bn, cg, splits, kb_per; size_t part_bytes; double t; };
 
 // The cheapest of the five tiles and of the ways to split the sum, by a model in microseconds: a block of 64 terms of a tile (measured
 // at 8192 x 4096 x 4096: 178 us with 256 x 256 tiles of CTA pairs; the narrow tiles wait for operands, not for the tensor cores), the
 // tiles a unit (CTA or CTA pair) takes in turn, 4.1 us for launch, filling the pipeline and the last tile's epilogue, and for split sums the
 // partial results' way through L2 and a second launch.
-Plan plan_product(long long I, int J, long long K) {
+// partial: the results stay fp32 sums in scratch even if the sum is not split.
+Plan plan_product(long long I, int J, long long K, bool partial = false) {
   struct Opt { int bn, cg; double kb; };
   static const Opt opts[5] = {{256, 2, 0.40}, {256, 1, 0.45}, {128, 1, 0.29}, {128, 2, 0.29}, {64, 1, 0.28}};
   const long long n_kb = (K + BK_TERMS - 1) / BK_TERMS;
@@ -259,16 +264,19 @@ Plan plan_product(long long I, int J, long long K) {
       const long long per = (n_kb + s - 1) / s;
       if (s > 1 && ((s - 1) * per >= n_kb || (size_t)s * I * Jp * 4 > (256u << 20))) continue;
       double t = (double)((tiles * s + units - 1) / units) * per * o.kb + 4.1;
-      if (s > 1) t += 2.5 + (double)s * I * Jp * 8.0 / 6e6;
+      if (s > 1 || partial) t += 2.5 + (double)s * I * Jp * 8.0 / 6e6;
       if (t < best_t) {
         best_t = t;
-        best = Plan{o.bn, o.cg, s, (int)per, s > 1 ? round256((size_t)s * I * Jp * 4) : 0};
+        best = Plan{o.bn, o.cg, s, (int)per, s > 1 || partial ? round256((size_t)s * I * Jp * 4) : 0, t};
       }
       if (tiles * s >= 2 * units) break;
     }
   }
   return best;
 }
+
+// The same for a product of pieces: six passes over the terms.
+Plan plan_pieces(long long I, int J, long long K) { return plan_product(I, J, split3::PAIRS * ((K + BK_TERMS - 1) / BK_TERMS * BK_TERMS), true); }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -333,14 +341,20 @@ int* status_word(int device) {
 }
 
 // C[I][J] = sum_t A(i, t) B(j, t) for stored operands; a_mn / b_mn: the operand is stored [t][i] / [t][j].
-int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, int J, long long K, const Result& r, float* part, int sms, int device,
-               cudaStream_t s) {
-  const Plan pl = plan_product(I, J, K);
+// pieces: the operands are fp32 in three pieces each, and the result is left as the plan's partial sums.
+int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, int J, long long K, const Result& r, bool pieces, float* part, int sms,
+               int device, cudaStream_t s) {
+  const Plan pl = pieces ? plan_pieces(I, J, K) : plan_product(I, J, K);
   const int Jp = (J + 3) / 4 * 4;
   dense::Args p = {};
   p.a_mn = a_mn; p.b_mn = b_mn;
   p.I = I; p.J = J;
-  p.n_kb = (int)((K + BK_TERMS - 1) / BK_TERMS);
+  p.kb_pass = (int)((K + BK_TERMS - 1) / BK_TERMS);
+  p.n_kb = p.kb_pass;
+  if (pieces) {
+    p.n_kb *= split3::PAIRS;
+    p.a_step = (int)(a.rows / 3); p.b_step = (int)(b.rows / 3);
+  }
   p.splits = pl.splits; p.kb_per = pl.kb_per;
   p.n_it = (I + 128 * pl.cg - 1) / (128 * pl.cg);
   p.n_jt = (J + pl.bn - 1) / pl.bn;
@@ -351,7 +365,7 @@ int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, in
   if (!p.status) return fail(ABS_ECUDA, "cudaGetSymbolAddress(status) failed");
   CUtensorMap ma, mb, mo, mz;
   bool ok = matrix_map(&ma, a.p, a.rows, a.cols, a.ld, a_mn ? 64 : 128) && matrix_map(&mb, b.p, b.rows, b.cols, b.ld, b_mn ? 64 : pl.bn / pl.cg);
-  if (pl.splits > 1) {
+  if (pl.splits > 1 || pieces) {
     p.partial = 1;
     ok = ok && partial_map(&mo, part, I, J, Jp, pl.splits);
   } else {
@@ -370,7 +384,7 @@ int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, in
   if (!ok) return fail(ABS_ECUDA, "cuTensorMapEncodeTiled failed");
   cudaError_t e = pl.cg == 2 ? (pl.bn == 256 ? launch_dense<256, 2>(ma, mb, mo, mz, p, sms, device, s) : launch_dense<128, 2>(ma, mb, mo, mz, p, sms, device, s)) : pl.bn == 256 ? launch_dense<256, 1>(ma, mb, mo, mz, p, sms, device, s)
                   : pl.bn == 128 ? launch_dense<128, 1>(ma, mb, mo, mz, p, sms, device, s) : launch_dense<64, 1>(ma, mb, mo, mz, p, sms, device, s);
-  if (e == cudaSuccess && pl.splits > 1) e = finish<__nv_bfloat16>(part, pl.splits, I, J, r, sms, s);
+  if (e == cudaSuccess && pl.splits > 1 && !pieces) e = finish<__nv_bfloat16>(part, pl.splits, I, J, r, Flags{}, sms, s);
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }
 
@@ -384,12 +398,12 @@ int pack(const void* src, long long rows, long long cols, long long ld, void* ds
 
 // ------------------------------------------------------------------ fp32 products
 
-struct FmaPlan { int bm, Q, splits, kb_per; size_t part_bytes; };
+struct FmaPlan { int bm, Q, splits, kb_per; size_t part_bytes; double t; };
 // 64 x 64 or 128 x 128 tiles, how many CTAs of a cluster share a tile's sum, and into how many parts that go through scratch it is cut
 // besides.  A block of 32 k takes a CTA that is alone on its SM 0.95 or 3.3 us, two of them together 1.7 or 5.8 us (4096^3: 54
 // TFLOP/s); a round of CTAs costs 3 to 5 us for filling and results, a microsecond more in clusters, parts their way through L2 and a
 // launch.  CLUSTERS: clusters of q CTAs, two per SM, that the GPU runs at a time (72 clusters of four 150 us, pairs 126).
-FmaPlan plan_fma(long long I, int J, int K) {
+FmaPlan plan_fma(long long I, int J, int K, int most = 64) {
   static const int CLUSTERS[9] = {0, 296, 148, 93, 71, 56, 45, 37, 33};
   FmaPlan best = {};
   double least = 1e300;
@@ -398,7 +412,7 @@ FmaPlan plan_fma(long long I, int J, int K) {
   for (int bm : {64, 128}) {
     const long long tiles = (I + bm - 1) / bm * ((J + bm - 1) / bm);
     const double one = bm == 64 ? 0.95 : 3.3, two = bm == 64 ? 1.7 : 5.8;
-    for (int split = 1; split <= 64; split *= 2) {
+    for (int split = 1; split <= most; split *= 2) {
       const size_t bytes = split > 1 ? round256((size_t)split * (I * Jp + J) * 4) : 0;
       if (split > 1 && (bytes > (64u << 20) || tiles * (split / 2) > 2 * PLAN_SMS)) break;
       for (int q = 1; q <= 8; ++q) {
@@ -408,7 +422,7 @@ FmaPlan plan_fma(long long I, int J, int K) {
         const double around = (bm == 64 ? 3.0 : 5.0) + (q > 1 ? 1.0 : 0.0);
         const double last = rest == 0 ? 0.0 : (rest * q > PLAN_SMS - 12 ? two : one) * per + around;
         const double t = (double)full * (two * per + around) + last + (split > 1 ? 2.5 + (double)bytes * 2.0 / 6e6 : 0.0);
-        if (t < least) { least = t; best = FmaPlan{bm, q, split, per, bytes}; }
+        if (t < least) { least = t; best = FmaPlan{bm, q, split, per, bytes, t}; }
       }
     }
   }
@@ -456,10 +470,58 @@ int fma_product(fp32::Args p, const FmaPlan& pl, long long I, int J, int K, int 
                   : launch(fma_fn<128>(in_kernel), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<128, 128>::SMEM, pl.Q, s, p);
   if (e == cudaSuccess && pl.splits > 1) {
     const Result r = {whole.bias, whole.res, whole.ldr, whole.out, whole.ldo, whole.pre, whole.ldp, act};
-    e = finish<float>(part, pl.splits, (int)I, J, r, sms, s);
+    e = finish<float>(part, pl.splits, (int)I, J, r, Flags{}, sms, s);
     if (e == cudaSuccess && whole.colsum)
       e = launch(column_kernel<float>, dim3((unsigned)((J + 31) / 32)), 256, 0, 1, s, (const float*)p.colsum, pl.splits, J, (void*)whole.colsum);
   }
+  return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
+}
+
+// ------------------------------------------------------------------ fp32 products on the tensor cores
+
+constexpr int SPLIT_BLOCKS = 4 * PLAN_SMS;
+constexpr size_t FLAG_BYTES = (SPLIT_BLOCKS * 4 + 255) / 256 * 256;
+long long rows64(long long rows) { return (rows + 63) / 64 * 64; }
+size_t piece_bytes(long long rows, int cols) { return round256((size_t)rows64(rows) * ((cols + 7) / 8 * 8) * 6); }
+constexpr double SPARE_TIME = 3.0;                        // the plain product's launch, which finds nothing to do
+double split_time(size_t bytes) { return 3.0 + (double)bytes * (10.0 / 6.0) / 4e6; }
+// matrices whose pieces and results stay well inside scratch and the copies' coordinates
+bool pieces_fit(long long I, int J, const Plan& pl, size_t bytes) {
+  return bytes <= (2ull << 30) && pl.part_bytes <= (1ull << 30) && (size_t)I * ((J + 3) / 4 * 4) <= (1ull << 28);
+}
+
+split3::Matrix in_pieces(const void* src, long long ld, long long rows, int cols, void* dst) {
+  split3::Matrix m = {};
+  m.src = (const float*)src; m.ld = ld; m.rows = rows; m.cols = cols;
+  m.dst = (__nv_bfloat16*)dst; m.rows_p = (uint32_t)rows64(rows); m.cols_p = (cols + 7) / 8 * 8;
+  m.vec = (uintptr_t)src % 16 == 0 && ld % 4 == 0;
+  m.per_row = Divisor((uint32_t)(m.cols_p / 8));
+  return m;
+}
+cudaError_t split(std::initializer_list<split3::Matrix> ms, Flags* flags, cudaStream_t s) {
+  split3::Args a = {};
+  uint32_t n = 0, i = 0;
+  for (const split3::Matrix& m : ms) {
+    a.m[i] = m;
+    n += m.rows_p * (uint32_t)(m.cols_p / 8);            // (at most 2^27 groups in 2 GB)
+    a.m[i++].end = n;
+  }
+  a.n = n;
+  a.flags = flags->p;
+  const uint32_t blocks = (n + 255) / 256;
+  flags->n = (int)(blocks < SPLIT_BLOCKS ? blocks : SPLIT_BLOCKS);
+  return launch(split3::split_kernel, dim3((unsigned)flags->n), 256, 0, 1, s, a);
+}
+// C = epilogue(A B) from pieces: the product, then the plain one, which works only if a flag is raised, then the epilogue, which works otherwise.
+int pieces_product(const split3::Matrix& a, int a_mn, const split3::Matrix& b, int b_mn, fp32::Args plain, int I, int J, int K, int act, const Flags& flags,
+                   float* part, int sms, int device, cudaStream_t s) {
+  const Operand oa = {a.dst, 3ll * a.rows_p, a.cols_p, a.cols_p}, ob = {b.dst, 3ll * b.rows_p, b.cols_p, b.cols_p};
+  const Result r = {plain.bias, plain.res, plain.ldr, plain.out, plain.ldo, plain.pre, plain.ldp, act};
+  int rc = tc_product(oa, a_mn, ob, b_mn, I, J, K, r, true, part, sms, device, s);
+  if (rc != ABS_OK) return rc;
+  plain.flags = flags.p; plain.n_flags = flags.n;
+  if ((rc = fma_product(plain, plan_fma(I, J, K, 1), I, J, K, act, nullptr, sms, device, s)) != ABS_OK) return rc;
+  const cudaError_t e = finish<float>(part, plan_pieces(I, J, K).splits, I, J, r, flags, sms, s);
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }
 
@@ -531,12 +593,21 @@ int check_matrix(const char* name, const void* p, long long rows, long long cols
 }
 
 // Scratch of a call.  need_*: the operand is copied to a pitch that TMA can address (bf16).
-struct FwdPlan { size_t x, w, part, total; FmaPlan fma; };
+struct FwdPlan { size_t x, w, part, total, flags; FmaPlan fma; bool pieces; };
 FwdPlan fwd_plan(long long rows, int n_in, int n_out, int dtype, bool pack_x, bool pack_w) {
   FwdPlan f = {};
   if (dtype == ABS_FP32) {
     f.fma = plan_fma(rows, n_out, n_in);
     f.total = f.fma.part_bytes;
+    const Plan pl = plan_pieces(rows, n_out, n_in);
+    const size_t bx = piece_bytes(rows, n_in), bw = piece_bytes(n_in, n_out);
+    f.pieces = pieces_fit(rows, n_out, pl, bx + bw) && pl.t + SPARE_TIME + split_time(bx + bw) < f.fma.t;
+    if (f.pieces) {
+      f.w = bx;
+      f.part = bx + bw;
+      f.flags = f.part + pl.part_bytes;
+      f.total = f.flags + FLAG_BYTES;
+    }
     return f;
   }
   f.w = pack_x ? pack_bytes(rows, n_in) : 0;
@@ -544,7 +615,7 @@ FwdPlan fwd_plan(long long rows, int n_in, int n_out, int dtype, bool pack_x, bo
   f.total = f.part + plan_product(rows, n_out, n_in).part_bytes;
   return f;
 }
-struct GradPlan { size_t dz, sums, x, w, part, total; long long ld_dz; int chunk, chunks; FmaPlan dx, dw; };
+struct GradPlan { size_t dz, sums, x, w, part, total; long long ld_dz; int chunk, chunks; FmaPlan dx, dw; bool pieces; size_t pz, px, pw, flags; };
 GradPlan grad_plan(long long rows, int n_in, int n_out, int dtype, bool need_dz, bool pack_x, bool pack_w) {
   GradPlan g = {};
   const size_t esz = dtype == ABS_FP32 ? 4 : 2;
@@ -563,6 +634,16 @@ GradPlan grad_plan(long long rows, int n_in, int n_out, int dtype, bool need_dz,
   if (dtype == ABS_FP32) {
     g.dx = plan_fma(rows, n_in, n_out); g.dw = plan_fma(n_in, n_out, (int)rows);
     a = g.dx.part_bytes; b = g.dw.part_bytes;
+    const Plan tx = plan_pieces(rows, n_in, n_out), tw = plan_pieces(n_in, n_out, rows);
+    const size_t bz = piece_bytes(rows, n_out), bx = piece_bytes(rows, n_in), bw = piece_bytes(n_in, n_out);
+    g.pieces = pieces_fit(rows, n_in, tx, bz + bx + bw) && pieces_fit(n_in, n_out, tw, 0) &&
+               tx.t + tw.t + 2 * SPARE_TIME + split_time(bz + bx + bw) < g.dx.t + g.dw.t;
+    if (g.pieces) {
+      g.pz = g.part; g.px = g.pz + bz; g.pw = g.px + bx;
+      g.flags = g.pw + bw;
+      g.part = g.flags + FLAG_BYTES;
+      a = tx.part_bytes; b = tw.part_bytes;
+    }
   } else {
     a = plan_product(rows, n_in, n_out).part_bytes; b = plan_product(n_in, n_out, rows).part_bytes;
   }
@@ -622,6 +703,14 @@ extern "C" int abs_linear(const void* x, long long ldx, const void* w, long long
     p.b = (const float*)w; p.b_k = ldw; p.b_j = 1;
     p.bias = (const float*)bias; p.res = (const float*)residual; p.out = (float*)y; p.pre = (float*)pre;
     p.ldr = ldr; p.ldo = ldy; p.ldp = ldp;
+    if (f.pieces) {
+      char* sc = (char*)scratch;
+      Flags flags = {(uint32_t*)(sc + f.flags), 0};
+      const split3::Matrix mx = in_pieces(x, ldx, rows, n_in, sc), mw = in_pieces(w, ldw, n_in, n_out, sc + f.w);
+      const cudaError_t e = split({mx, mw}, &flags, s);
+      if (e != cudaSuccess) return fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
+      return pieces_product(mx, 0, mw, 1, p, (int)rows, n_out, n_in, act, flags, (float*)(sc + f.part), sms, device, s);
+    }
     return fma_product(p, f.fma, rows, n_out, n_in, act, (float*)scratch, sms, device, s);
   }
   char* sc = (char*)scratch;
@@ -635,7 +724,7 @@ extern "C" int abs_linear(const void* x, long long ldx, const void* w, long long
     b.p = sc + f.w; b.ld = (n_out + 7) / 8 * 8;
   }
   const Result r = {bias, residual, ldr, y, ldy, pre, ldp, act};
-  return tc_product(a, 0, b, 1, (int)rows, n_out, n_in, r, (float*)(sc + f.part), sms, device, s);
+  return tc_product(a, 0, b, 1, (int)rows, n_out, n_in, r, false, (float*)(sc + f.part), sms, device, s);
 }
 
 extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, long long ldx, const void* w, long long ldw,
@@ -680,7 +769,7 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
   char* sc = (char*)scratch;
   const void* dz = need_dz ? sc + g.dz : dy;
   const long long lddz = need_dz ? g.ld_dz : lddy;
-  const bool with_dw = !bf16 && dw && db;              // the column sums come with the product
+  const bool with_dw = !bf16 && !g.pieces && dw && db; // the column sums come with the product
   float* part = db && !with_dw ? (float*)(sc + g.sums) : nullptr;
   cudaError_t e = cudaSuccess;
   if (need_dz || part) {
@@ -698,12 +787,22 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
                (const float*)part, g.chunks, n_out, db);
   if (e != cudaSuccess) return fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
   if (!bf16) {
+    const split3::Matrix none = {};
+    const split3::Matrix mz = in_pieces(dz, lddz, rows, n_out, sc + g.pz), mx = dw ? in_pieces(x, ldx, rows, n_in, sc + g.px) : none;
+    const split3::Matrix mw = dx ? in_pieces(w, ldw, n_in, n_out, sc + g.pw) : none;
+    Flags flags = {(uint32_t*)(sc + g.flags), 0};
+    if (g.pieces && (dx || dw)) {
+      e = dx && dw ? split({mz, mx, mw}, &flags, s) : dw ? split({mz, mx}, &flags, s) : split({mz, mw}, &flags, s);
+      if (e != cudaSuccess) return fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
+    }
     if (dx) {
       fp32::Args p = {};
       p.a = (const float*)dz; p.a_i = lddz; p.a_k = 1;
       p.b = (const float*)w; p.b_k = 1; p.b_j = ldw;
       p.out = (float*)dx; p.ldo = lddx;
-      if ((rc = fma_product(p, g.dx, rows, n_in, n_out, ABS_ACT_NONE, (float*)(sc + g.part), sms, device, s)) != ABS_OK) return rc;
+      if (g.pieces) rc = pieces_product(mz, 0, mw, 0, p, (int)rows, n_in, n_out, ABS_ACT_NONE, flags, (float*)(sc + g.part), sms, device, s);
+      else rc = fma_product(p, g.dx, rows, n_in, n_out, ABS_ACT_NONE, (float*)(sc + g.part), sms, device, s);
+      if (rc != ABS_OK) return rc;
     }
     if (dw) {
       fp32::Args p = {};
@@ -711,7 +810,9 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
       p.b = (const float*)dz; p.b_k = lddz; p.b_j = 1;
       p.out = (float*)dw; p.ldo = lddw;
       p.colsum = with_dw ? (float*)db : nullptr;
-      if ((rc = fma_product(p, g.dw, n_in, n_out, (int)rows, ABS_ACT_NONE, (float*)(sc + g.part), sms, device, s)) != ABS_OK) return rc;
+      if (g.pieces) rc = pieces_product(mx, 1, mz, 1, p, n_in, n_out, (int)rows, ABS_ACT_NONE, flags, (float*)(sc + g.part), sms, device, s);
+      else rc = fma_product(p, g.dw, n_in, n_out, (int)rows, ABS_ACT_NONE, (float*)(sc + g.part), sms, device, s);
+      if (rc != ABS_OK) return rc;
     }
     return ABS_OK;
   }
@@ -724,7 +825,7 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
       ow.p = sc + g.w; ow.ld = (n_out + 7) / 8 * 8;
     }
     const Result r = {nullptr, nullptr, 0, dx, lddx, nullptr, 0, ABS_ACT_NONE};
-    if ((rc = tc_product(od, 0, ow, 0, (int)rows, n_in, n_out, r, split, sms, device, s)) != ABS_OK) return rc;
+    if ((rc = tc_product(od, 0, ow, 0, (int)rows, n_in, n_out, r, false, split, sms, device, s)) != ABS_OK) return rc;
   }
   if (dw) {
     Operand ox = {x, rows, n_in, tma_pitch(rows, n_in, ldx)};
@@ -733,7 +834,7 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
       ox.p = sc + g.x; ox.ld = (n_in + 7) / 8 * 8;
     }
     const Result r = {nullptr, nullptr, 0, dw, lddw, nullptr, 0, ABS_ACT_NONE};
-    if ((rc = tc_product(ox, 1, od, 1, n_in, n_out, rows, r, split, sms, device, s)) != ABS_OK) return rc;
+    if ((rc = tc_product(ox, 1, od, 1, n_in, n_out, rows, r, false, split, sms, device, s)) != ABS_OK) return rc;
   }
   return ABS_OK;
 }

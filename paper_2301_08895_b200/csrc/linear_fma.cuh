@@ -11,6 +11,7 @@
 // kernel adds.
 #pragma once
 #include "layerops.cuh"
+#include "linear_split.cuh"
 
 namespace absb {
 namespace fp32 {
@@ -27,6 +28,7 @@ struct Args {
   float* colsum;                         // sums of B's columns (null: none), by the CTAs of the first row tile
   long long out_step; int col_step;      // part number s of a sum cut in parts goes to out + s out_step, colsum + s col_step
   layer::Divisor by_Q, by_njt, by_tiles; // by_tiles: tiles of one part
+  const uint32_t* flags; int n_flags;    // work only if one of these is raised (null: always)
 };
 
 template <int BM, int BN> struct Cfg {
@@ -124,6 +126,7 @@ __global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Args
   const int j0 = (int)(tile - it * p.by_njt.d) * BN;
   const int kb0 = ((int)part * p.Q + rank) * p.kb_per, nkb = min(p.kb_per, p.n_kb - kb0);
   grid_dependency_sync();
+  if (p.flags && !split3::any_flag(p.flags, p.n_flags)) return;    // (the whole grid alike)
 
   const int X = (int)min((long long)BM, p.I - i0), Y = min(BN, p.J - j0);
   const Mover<BM, false> ma(p.a, p.a_i, p.a_k, i0, X);

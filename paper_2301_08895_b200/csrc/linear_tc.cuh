@@ -4,7 +4,7 @@
 //   operand     dX[m][k] = sum_n dZ[m][n] W[k][n]                             both: n contiguous
 //   weights     dW[k][n] = sum_m X[m][k] dZ[m][n]                             neither: the sum runs over rows
 //
-// are one kernel: C[i][j] = sum_t A(i, t) B(j, t), each operand either with t contiguous ("K-major": one box of 64 t per
+// (and in fp32 as six passes over three pieces of each operand, see linear_split.cuh) are one kernel: C[i][j] = sum_t A(i, t) B(j, t), each operand either with t contiguous ("K-major": one box of 64 t per
 // 128 rows) or with i (j) contiguous ("MN-major": boxes of 64 columns x 64 t).  Both arrive by TMA in the 128-byte swizzle
 // that tcgen05.mma reads; sizes that do not fill a tile are filled with zeros by the copies and clipped by the stores.
 //
@@ -15,6 +15,7 @@
 // Every wait is bounded: on expiry the CTA raises the operations' status word, drains its copies, frees tensor memory and returns.
 #pragma once
 #include "layerops.cuh"
+#include "linear_split.cuh"
 #include "tcprim.cuh"
 
 namespace absb {
@@ -29,6 +30,7 @@ struct Args {
   int a_mn, b_mn;                        // operand layouts: 0 K-major, 1 MN-major
   int I, J, n_kb;                        // rows and columns of C; blocks of 64 terms of the sum
   int splits, kb_per;                    // tiles that share a sum, blocks of each
+  int kb_pass, a_step, b_step;           // blocks of one pair of pieces; rows from a piece to the next (0: bf16, one pass)
   int n_it, n_jt, n_tiles;
   // final results (splits = 1)
   const __nv_bfloat16* bias; const __nv_bfloat16* res; __nv_bfloat16* out; __nv_bfloat16* pre;
@@ -177,6 +179,8 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
       for (int t = unit; t < p.n_tiles && ok; t += n_units) {
         const Tile c = tile_of(t);
         const int j0 = c.j0 + rank * BH;
+        int pass = c.kb0 / p.kb_pass, k0 = (c.kb0 - pass * p.kb_pass) * BK;
+        int ra = p.a_step * (int)(split3::A_PIECE >> 4 * pass & 15u), rb = p.b_step * (int)(split3::B_PIECE >> 4 * pass & 15u);
         for (int kb = 0; kb < c.n_kb; ++kb) {
           if (!mbar_wait(&empty[stage], phase ^ 1u, abort)) { ok = false; break; }
           uint8_t* sa = smem + (size_t)stage * C::STAGE_BYTES;
@@ -185,16 +189,22 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             mbar_expect_tx(&full[stage], CG * C::STAGE_BYTES);
             armed[stage] = (int)phase;
           }
-          const int k0 = (c.kb0 + kb) * BK;
           if (p.a_mn) {
-            for (int j = 0; j < BM / 64; ++j) load(sa + j * 8192, &map_a, stage, c.i0 + 64 * j, k0);
+            for (int j = 0; j < BM / 64; ++j) load(sa + j * 8192, &map_a, stage, c.i0 + 64 * j, k0 + ra);
           } else {
-            load(sa, &map_a, stage, k0, c.i0);
+            load(sa, &map_a, stage, k0, c.i0 + ra);
           }
           if (p.b_mn) {
-            for (int j = 0; j < BH / 64; ++j) load(sb + j * 8192, &map_b, stage, j0 + 64 * j, k0);
+            for (int j = 0; j < BH / 64; ++j) load(sb + j * 8192, &map_b, stage, j0 + 64 * j, k0 + rb);
           } else {
-            load(sb, &map_b, stage, k0, j0);
+            load(sb, &map_b, stage, k0, j0 + rb);
+          }
+          k0 += BK;
+          if (k0 == p.kb_pass * BK) {
+            k0 = 0;
+            ++pass;
+            ra = p.a_step * (int)(split3::A_PIECE >> 4 * pass & 15u);
+            rb = p.b_step * (int)(split3::B_PIECE >> 4 * pass & 15u);
           }
           if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
         }

@@ -314,6 +314,107 @@ def test_linear_fp32_long_sums(M, K, N, pad, offset):
     grad_case(M, K, N, False, gpu.ACT_RELU, pad=pad, offset=offset, seed=M, want=(True, False, False))
 
 
+def takes_pieces(M, K, N, grad=False):
+    """Whether the call's scratch has room for three bf16 pieces of each of its matrices."""
+    pieces = 6 * (M * K + K * N + (M * N if grad else 0))
+    return gpu.linear_scratch_bytes(M, K, N, gpu.ACT_NONE, gpu.FP32, grad) > pieces
+
+
+@pytest.mark.parametrize("pad,offset", [(0, 0), (1, 0), (3, 5), (8, 8)])
+@pytest.mark.parametrize("M,K,N", [(1037, 785, 501), (512, 1024, 1024), (8192, 784, 256), (1100, 701, 520), (2500, 2500, 641), (300, 10000, 300)])
+def test_linear_fp32_in_pieces(M, K, N, pad, offset):
+    """Six products of bf16 pieces: what they leave out is below 2^-23 of |x| |w|, one more term in the bound's K + 4; the tensor cores add 16
+    products at a time, K / 16 such additions of the results' size and 5 K / 16 of at most 2^-7 of it."""
+    assert takes_pieces(M, K, N)
+    linear_case(M, K, N, False, gpu.ACT_SILU, True, True, pad=pad, offset=offset, seed=K)
+    linear_case(M, K, N, False, gpu.ACT_NONE, False, False, bias=False, pad=pad, offset=offset, seed=K)
+    linear_case(M, K, N, False, gpu.ACT_RELU, True, False, pad=pad, offset=offset, seed=K, in_place=True)
+
+
+@pytest.mark.parametrize("pad,offset", [(0, 0), (1, 0), (8, 8)])
+@pytest.mark.parametrize("M,K,N", [(2048, 1024, 1024), (1037, 785, 501), (20000, 400, 120), (777, 2049, 1300)])
+def test_linear_grad_fp32_in_pieces(M, K, N, pad, offset):
+    assert takes_pieces(M, K, N, True)
+    grad_case(M, K, N, False, gpu.ACT_GELU, pad=pad, offset=offset, seed=M)
+    for want in ((True, False, False), (False, True, False), (False, False, True), (True, False, True), (False, True, True)):
+        grad_case(M, K, N, False, gpu.ACT_NONE, pad=pad, offset=offset, seed=M, want=want)
+
+
+def test_linear_fp32_of_what_pieces_cannot_hold():
+    """Infinities, NaN, the largest and the smallest numbers: the results of fp32 all the same, in the forward and the backward products."""
+    torch = _torch()
+    M, K, N = 520, 1024, 1030
+    assert takes_pieces(M, K, N) and takes_pieces(M, K, N, True)
+    top = torch.finfo(torch.float32).max
+    for bad in (float("inf"), -float("inf"), float("nan"), top, -top, 2.0 ** -112, 1e-42, 0.0):
+        for scale in (1.0, 2.0 ** -100):
+            g = gen(7)
+            x, w, r = randn(g, M, K), randn(g, K, N, scale=2.0 ** -20), randn(g, M, N)
+            x = x * scale
+            x[17, 33] = bad
+            w[40, 21] = 0.0
+            y = r.clone()
+            gpu.linear(x, w, None, y, y)
+            x64, w64, r64 = x.double(), w.double(), r.double()
+            want = x64 @ w64 + r64
+            tol = 1.2 * (K + 4) * E23 * (x64.abs() @ w64.abs()) + 2 * E23 * (r64.abs() + want.abs()) + 2.0 ** -126
+            inf = torch.isinf(want)
+            assert torch.equal(torch.isnan(y), torch.isnan(want)) and torch.equal(y[inf].double(), want[inf])
+            ok = torch.isfinite(want)
+            within(y[ok], want[ok], tol[ok])
+    for value in (2.0 ** -112, 2.0 ** -120):             # all of a matrix below what pieces hold
+        g = gen(8)
+        x, w, dy = randn(g, M, K) * value, randn(g, K, N) * 2.0 ** 90, randn(g, M, N) * value
+        y, dx, dw = torch.empty(M, N, device="cuda"), torch.empty_like(x), torch.empty_like(w)
+        gpu.linear(x, w, None, None, y)
+        within(y, x.double() @ w.double(), 1.2 * (K + 4) * E23 * (x.double().abs() @ w.double().abs()))
+        gpu.linear_grad(dy, randn(g, M, K), w, None, dx, None, None)
+        within(dx, dy.double() @ w.double().T, 1.2 * (N + 4) * E23 * (dy.double().abs() @ w.double().abs().T))
+        xx = randn(g, M, K) * 2.0 ** 90
+        gpu.linear_grad(dy, xx, w, None, None, dw, None)
+        within(dw, xx.double().T @ dy.double(), 1.2 * (M + 4) * E23 * (xx.double().abs().T @ dy.double().abs()))
+
+
+def test_linear_fp32_in_pieces_captured_and_on_another_stream():
+    """The flags of a step are its own: a replay with an infinity in x, and one without it again."""
+    torch = _torch()
+    g = gen(11)
+    M, K, N = 600, 1024, 1024
+    x, w, dy = randn(g, M, K), randn(g, K, N), randn(g, M, N)
+    y, dx, dw, db = torch.empty(M, N, device="cuda"), torch.empty_like(x), torch.empty_like(w), torch.empty(N, device="cuda")
+    size = max(gpu.linear_scratch_bytes(M, K, N, dtype=gpu.FP32), gpu.linear_scratch_bytes(M, K, N, dtype=gpu.FP32, grad=True))
+    scratch = torch.empty(size, dtype=torch.uint8, device="cuda")
+    outs = (y, dx, dw, db)
+
+    def step():
+        gpu.linear(x, w, None, None, y, scratch=scratch)
+        gpu.linear_grad(dy, x, w, None, dx, dw, db, scratch=scratch)
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for t in outs:
+            t.fill_(float("nan"))
+        step()
+    side.synchronize()
+    assert all(torch.equal(t, v) for t, v in zip(outs, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    keep = float(x[5, 6])
+    for value in (keep, float("inf"), keep):
+        x[5, 6] = value
+        graph.replay()
+        torch.cuda.synchronize()
+        if value == keep:
+            assert all(torch.equal(t, v) for t, v in zip(outs, want))
+        else:
+            assert not torch.isfinite(y[5]).any() and bool(torch.isfinite(y[6:]).all()) and bool(torch.isfinite(y[:5]).all())
+            assert not torch.isfinite(dw[6]).any() and bool(torch.isfinite(dw[7:]).all()) and bool(torch.isfinite(dx).all())
+
+
 def test_linear_fp32_parts_in_a_captured_step():
     """The scratch of a call serves the next one on its stream: forward, gradients and forward again in one graph, replayed, give the same bits."""
     torch = _torch()
