@@ -159,12 +159,10 @@ struct FinishArgs {
   long long ldr, ldo, ldp;
   Divisor quads;                         // groups of four columns per row
   uint32_t n;                            // groups
-  const uint32_t* flags; int n_flags;    // no work if one of these is raised
 };
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256) finish_kernel(FinishArgs a) {
   grid_dependency_sync();
-  if (a.flags && split3::any_flag(a.flags, a.n_flags)) return;
   for (uint32_t q = blockIdx.x * 256u + threadIdx.x; q < a.n; q += gridDim.x * 256u) {
     const uint32_t i = a.quads.div(q), j = 4u * (q - i * a.quads.d);
     const float* p = a.part + (size_t)i * a.Jp + j;
@@ -227,13 +225,11 @@ struct Result {
 };
 
 typedef void (*FinishFn)(FinishArgs);
-struct Flags { uint32_t* p; int n; };
-template <typename T> cudaError_t finish(const float* part, int splits, int I, int J, const Result& r, const Flags& flags, int sms, cudaStream_t s) {
+template <typename T> cudaError_t finish(const float* part, int splits, int I, int J, const Result& r, int sms, cudaStream_t s) {
   FinishArgs f = {};
   f.part = part; f.splits = splits; f.I = I; f.J = J; f.Jp = (J + 3) / 4 * 4;
   f.bias = r.bias; f.res = r.res; f.out = r.out; f.pre = r.pre;
   f.ldr = r.ldr; f.ldo = r.ldo; f.ldp = r.ldp;
-  f.flags = flags.p; f.n_flags = flags.n;
   f.quads = Divisor((uint32_t)(f.Jp / 4));
   f.n = (uint32_t)((size_t)I * (f.Jp / 4));              // (partial results hold at most 2^28 floats)
   const unsigned blocks = (f.n + 255) / 256;
@@ -342,9 +338,8 @@ int* status_word(int device) {
 
 // C[I][J] = sum_t A(i, t) B(j, t) for stored operands; a_mn / b_mn: the operand is stored [t][i] / [t][j].
 // pieces: the operands are fp32 in three pieces each, and the result is left as the plan's partial sums.
-int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, int J, long long K, const Result& r, bool pieces, float* part, int sms,
-               int device, cudaStream_t s) {
-  const Plan pl = pieces ? plan_pieces(I, J, K) : plan_product(I, J, K);
+int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, int J, long long K, const Result& r, const Plan& pl, bool pieces, float* part,
+               int sms, int device, cudaStream_t s) {
   const int Jp = (J + 3) / 4 * 4;
   dense::Args p = {};
   p.a_mn = a_mn; p.b_mn = b_mn;
@@ -384,7 +379,7 @@ int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, in
   if (!ok) return fail(ABS_ECUDA, "cuTensorMapEncodeTiled failed");
   cudaError_t e = pl.cg == 2 ? (pl.bn == 256 ? launch_dense<256, 2>(ma, mb, mo, mz, p, sms, device, s) : launch_dense<128, 2>(ma, mb, mo, mz, p, sms, device, s)) : pl.bn == 256 ? launch_dense<256, 1>(ma, mb, mo, mz, p, sms, device, s)
                   : pl.bn == 128 ? launch_dense<128, 1>(ma, mb, mo, mz, p, sms, device, s) : launch_dense<64, 1>(ma, mb, mo, mz, p, sms, device, s);
-  if (e == cudaSuccess && pl.splits > 1 && !pieces) e = finish<__nv_bfloat16>(part, pl.splits, I, J, r, Flags{}, sms, s);
+  if (e == cudaSuccess && pl.splits > 1 && !pieces) e = finish<__nv_bfloat16>(part, pl.splits, I, J, r, sms, s);
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }
 
@@ -470,7 +465,7 @@ int fma_product(fp32::Args p, const FmaPlan& pl, long long I, int J, int K, int 
                   : launch(fma_fn<128>(in_kernel), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<128, 128>::SMEM, pl.Q, s, p);
   if (e == cudaSuccess && pl.splits > 1) {
     const Result r = {whole.bias, whole.res, whole.ldr, whole.out, whole.ldo, whole.pre, whole.ldp, act};
-    e = finish<float>(part, pl.splits, (int)I, J, r, Flags{}, sms, s);
+    e = finish<float>(part, pl.splits, (int)I, J, r, sms, s);
     if (e == cudaSuccess && whole.colsum)
       e = launch(column_kernel<float>, dim3((unsigned)((J + 31) / 32)), 256, 0, 1, s, (const float*)p.colsum, pl.splits, J, (void*)whole.colsum);
   }
@@ -483,13 +478,13 @@ constexpr int SPLIT_BLOCKS = 4 * PLAN_SMS;
 constexpr size_t FLAG_BYTES = (SPLIT_BLOCKS * 4 + 255) / 256 * 256;
 long long rows64(long long rows) { return (rows + 63) / 64 * 64; }
 size_t piece_bytes(long long rows, int cols) { return round256((size_t)rows64(rows) * ((cols + 7) / 8 * 8) * 6); }
-constexpr double SPARE_TIME = 3.0;                        // the plain product's launch, which finds nothing to do
 double split_time(size_t bytes) { return 3.0 + (double)bytes * (10.0 / 6.0) / 4e6; }
 // matrices whose pieces and results stay well inside scratch and the copies' coordinates
 bool pieces_fit(long long I, int J, const Plan& pl, size_t bytes) {
   return bytes <= (2ull << 30) && pl.part_bytes <= (1ull << 30) && (size_t)I * ((J + 3) / 4 * 4) <= (1ull << 28);
 }
 
+struct Flags { uint32_t* p; int n; };
 split3::Matrix in_pieces(const void* src, long long ld, long long rows, int cols, void* dst) {
   split3::Matrix m = {};
   m.src = (const float*)src; m.ld = ld; m.rows = rows; m.cols = cols;
@@ -512,17 +507,17 @@ cudaError_t split(std::initializer_list<split3::Matrix> ms, Flags* flags, cudaSt
   flags->n = (int)(blocks < SPLIT_BLOCKS ? blocks : SPLIT_BLOCKS);
   return launch(split3::split_kernel, dim3((unsigned)flags->n), 256, 0, 1, s, a);
 }
-// C = epilogue(A B) from pieces: the product, then the plain one, which works only if a flag is raised, then the epilogue, which works otherwise.
-int pieces_product(const split3::Matrix& a, int a_mn, const split3::Matrix& b, int b_mn, fp32::Args plain, int I, int J, int K, int act, const Flags& flags,
-                   float* part, int sms, int device, cudaStream_t s) {
+// C = epilogue(A B) from pieces: their product, then the plain kernel, which only adds the epilogue unless a flag is raised.
+int pieces_product(const split3::Matrix& a, int a_mn, const split3::Matrix& b, int b_mn, fp32::Args plain, const Plan& pl, int I, int J, int K, int act,
+                   const Flags& flags, float* part, int sms, int device, cudaStream_t s) {
   const Operand oa = {a.dst, 3ll * a.rows_p, a.cols_p, a.cols_p}, ob = {b.dst, 3ll * b.rows_p, b.cols_p, b.cols_p};
-  const Result r = {plain.bias, plain.res, plain.ldr, plain.out, plain.ldo, plain.pre, plain.ldp, act};
-  int rc = tc_product(oa, a_mn, ob, b_mn, I, J, K, r, true, part, sms, device, s);
+  const int rc = tc_product(oa, a_mn, ob, b_mn, I, J, K, Result{}, pl, true, part, sms, device, s);
   if (rc != ABS_OK) return rc;
   plain.flags = flags.p; plain.n_flags = flags.n;
-  if ((rc = fma_product(plain, plan_fma(I, J, K, 1), I, J, K, act, nullptr, sms, device, s)) != ABS_OK) return rc;
-  const cudaError_t e = finish<float>(part, plan_pieces(I, J, K).splits, I, J, r, flags, sms, s);
-  return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
+  plain.sums = part; plain.parts = pl.splits;
+  auto whole = [](const void* p, long long ld) { return !p || ((uintptr_t)p % 16 == 0 && ld % 4 == 0); };
+  plain.vec = whole(plain.res, plain.ldr) && whole(plain.out, plain.ldo) && whole(plain.pre, plain.ldp);
+  return fma_product(plain, plan_fma(I, J, K, 1), I, J, K, act, nullptr, sms, device, s);
 }
 
 // ------------------------------------------------------------------ few rows, few outputs
@@ -593,29 +588,30 @@ int check_matrix(const char* name, const void* p, long long rows, long long cols
 }
 
 // Scratch of a call.  need_*: the operand is copied to a pitch that TMA can address (bf16).
-struct FwdPlan { size_t x, w, part, total, flags; FmaPlan fma; bool pieces; };
+struct FwdPlan { size_t w, part, total, flags; Plan tc; FmaPlan fma; bool pieces; };   // (x comes first)
 FwdPlan fwd_plan(long long rows, int n_in, int n_out, int dtype, bool pack_x, bool pack_w) {
   FwdPlan f = {};
   if (dtype == ABS_FP32) {
     f.fma = plan_fma(rows, n_out, n_in);
     f.total = f.fma.part_bytes;
-    const Plan pl = plan_pieces(rows, n_out, n_in);
+    f.tc = plan_pieces(rows, n_out, n_in);
     const size_t bx = piece_bytes(rows, n_in), bw = piece_bytes(n_in, n_out);
-    f.pieces = pieces_fit(rows, n_out, pl, bx + bw) && pl.t + SPARE_TIME + split_time(bx + bw) < f.fma.t;
+    f.pieces = pieces_fit(rows, n_out, f.tc, bx + bw) && f.tc.t + split_time(bx + bw) < f.fma.t;
     if (f.pieces) {
       f.w = bx;
       f.part = bx + bw;
-      f.flags = f.part + pl.part_bytes;
+      f.flags = f.part + f.tc.part_bytes;
       f.total = f.flags + FLAG_BYTES;
     }
     return f;
   }
   f.w = pack_x ? pack_bytes(rows, n_in) : 0;
   f.part = f.w + (pack_w ? pack_bytes(n_in, n_out) : 0);
-  f.total = f.part + plan_product(rows, n_out, n_in).part_bytes;
+  f.tc = plan_product(rows, n_out, n_in);
+  f.total = f.part + f.tc.part_bytes;
   return f;
 }
-struct GradPlan { size_t dz, sums, x, w, part, total; long long ld_dz; int chunk, chunks; FmaPlan dx, dw; bool pieces; size_t pz, px, pw, flags; };
+struct GradPlan { size_t dz, sums, x, w, part, total; long long ld_dz; int chunk, chunks; FmaPlan dx, dw; Plan tx, tw; bool pieces; size_t pz, px, pw, flags; };
 GradPlan grad_plan(long long rows, int n_in, int n_out, int dtype, bool need_dz, bool pack_x, bool pack_w) {
   GradPlan g = {};
   const size_t esz = dtype == ABS_FP32 ? 4 : 2;
@@ -634,18 +630,21 @@ GradPlan grad_plan(long long rows, int n_in, int n_out, int dtype, bool need_dz,
   if (dtype == ABS_FP32) {
     g.dx = plan_fma(rows, n_in, n_out); g.dw = plan_fma(n_in, n_out, (int)rows);
     a = g.dx.part_bytes; b = g.dw.part_bytes;
-    const Plan tx = plan_pieces(rows, n_in, n_out), tw = plan_pieces(n_in, n_out, rows);
+    g.tx = plan_pieces(rows, n_in, n_out);
+    g.tw = plan_pieces(n_in, n_out, rows);
     const size_t bz = piece_bytes(rows, n_out), bx = piece_bytes(rows, n_in), bw = piece_bytes(n_in, n_out);
-    g.pieces = pieces_fit(rows, n_in, tx, bz + bx + bw) && pieces_fit(n_in, n_out, tw, 0) &&
-               tx.t + tw.t + 2 * SPARE_TIME + split_time(bz + bx + bw) < g.dx.t + g.dw.t;
+    g.pieces = pieces_fit(rows, n_in, g.tx, bz + bx + bw) && pieces_fit(n_in, n_out, g.tw, 0) &&
+               g.tx.t + g.tw.t + split_time(bz + bx + bw) < g.dx.t + g.dw.t;
     if (g.pieces) {
       g.pz = g.part; g.px = g.pz + bz; g.pw = g.px + bx;
       g.flags = g.pw + bw;
       g.part = g.flags + FLAG_BYTES;
-      a = tx.part_bytes; b = tw.part_bytes;
+      a = g.tx.part_bytes; b = g.tw.part_bytes;
     }
   } else {
-    a = plan_product(rows, n_in, n_out).part_bytes; b = plan_product(n_in, n_out, rows).part_bytes;
+    g.tx = plan_product(rows, n_in, n_out);
+    g.tw = plan_product(n_in, n_out, rows);
+    a = g.tx.part_bytes; b = g.tw.part_bytes;
   }
   g.total = g.part + (a > b ? a : b);
   return g;
@@ -709,22 +708,22 @@ extern "C" int abs_linear(const void* x, long long ldx, const void* w, long long
       const split3::Matrix mx = in_pieces(x, ldx, rows, n_in, sc), mw = in_pieces(w, ldw, n_in, n_out, sc + f.w);
       const cudaError_t e = split({mx, mw}, &flags, s);
       if (e != cudaSuccess) return fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
-      return pieces_product(mx, 0, mw, 1, p, (int)rows, n_out, n_in, act, flags, (float*)(sc + f.part), sms, device, s);
+      return pieces_product(mx, 0, mw, 1, p, f.tc, (int)rows, n_out, n_in, act, flags, (float*)(sc + f.part), sms, device, s);
     }
     return fma_product(p, f.fma, rows, n_out, n_in, act, (float*)scratch, sms, device, s);
   }
   char* sc = (char*)scratch;
   Operand a = {x, rows, n_in, tma_pitch(rows, n_in, ldx)}, b = {w, n_in, n_out, tma_pitch(n_in, n_out, ldw)};
   if (pack_x) {
-    if ((rc = pack(x, rows, n_in, ldx, sc + f.x, sms, s)) != ABS_OK) return rc;
-    a.p = sc + f.x; a.ld = (n_in + 7) / 8 * 8;
+    if ((rc = pack(x, rows, n_in, ldx, sc, sms, s)) != ABS_OK) return rc;
+    a.p = sc; a.ld = (n_in + 7) / 8 * 8;
   }
   if (pack_w) {
     if ((rc = pack(w, n_in, n_out, ldw, sc + f.w, sms, s)) != ABS_OK) return rc;
     b.p = sc + f.w; b.ld = (n_out + 7) / 8 * 8;
   }
   const Result r = {bias, residual, ldr, y, ldy, pre, ldp, act};
-  return tc_product(a, 0, b, 1, (int)rows, n_out, n_in, r, false, (float*)(sc + f.part), sms, device, s);
+  return tc_product(a, 0, b, 1, (int)rows, n_out, n_in, r, f.tc, false, (float*)(sc + f.part), sms, device, s);
 }
 
 extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, long long ldx, const void* w, long long ldw,
@@ -800,7 +799,7 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
       p.a = (const float*)dz; p.a_i = lddz; p.a_k = 1;
       p.b = (const float*)w; p.b_k = 1; p.b_j = ldw;
       p.out = (float*)dx; p.ldo = lddx;
-      if (g.pieces) rc = pieces_product(mz, 0, mw, 0, p, (int)rows, n_in, n_out, ABS_ACT_NONE, flags, (float*)(sc + g.part), sms, device, s);
+      if (g.pieces) rc = pieces_product(mz, 0, mw, 0, p, g.tx, (int)rows, n_in, n_out, ABS_ACT_NONE, flags, (float*)(sc + g.part), sms, device, s);
       else rc = fma_product(p, g.dx, rows, n_in, n_out, ABS_ACT_NONE, (float*)(sc + g.part), sms, device, s);
       if (rc != ABS_OK) return rc;
     }
@@ -810,7 +809,7 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
       p.b = (const float*)dz; p.b_k = lddz; p.b_j = 1;
       p.out = (float*)dw; p.ldo = lddw;
       p.colsum = with_dw ? (float*)db : nullptr;
-      if (g.pieces) rc = pieces_product(mx, 1, mz, 1, p, n_in, n_out, (int)rows, ABS_ACT_NONE, flags, (float*)(sc + g.part), sms, device, s);
+      if (g.pieces) rc = pieces_product(mx, 1, mz, 1, p, g.tw, n_in, n_out, (int)rows, ABS_ACT_NONE, flags, (float*)(sc + g.part), sms, device, s);
       else rc = fma_product(p, g.dw, n_in, n_out, (int)rows, ABS_ACT_NONE, (float*)(sc + g.part), sms, device, s);
       if (rc != ABS_OK) return rc;
     }
@@ -825,7 +824,7 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
       ow.p = sc + g.w; ow.ld = (n_out + 7) / 8 * 8;
     }
     const Result r = {nullptr, nullptr, 0, dx, lddx, nullptr, 0, ABS_ACT_NONE};
-    if ((rc = tc_product(od, 0, ow, 0, (int)rows, n_in, n_out, r, false, split, sms, device, s)) != ABS_OK) return rc;
+    if ((rc = tc_product(od, 0, ow, 0, (int)rows, n_in, n_out, r, g.tx, false, split, sms, device, s)) != ABS_OK) return rc;
   }
   if (dw) {
     Operand ox = {x, rows, n_in, tma_pitch(rows, n_in, ldx)};
@@ -834,7 +833,7 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
       ox.p = sc + g.x; ox.ld = (n_in + 7) / 8 * 8;
     }
     const Result r = {nullptr, nullptr, 0, dw, lddw, nullptr, 0, ABS_ACT_NONE};
-    if ((rc = tc_product(ox, 1, od, 1, n_in, n_out, rows, r, false, split, sms, device, s)) != ABS_OK) return rc;
+    if ((rc = tc_product(ox, 1, od, 1, n_in, n_out, rows, r, g.tw, false, split, sms, device, s)) != ABS_OK) return rc;
   }
   return ABS_OK;
 }

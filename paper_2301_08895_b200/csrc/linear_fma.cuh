@@ -28,7 +28,8 @@ struct Args {
   float* colsum;                         // sums of B's columns (null: none), by the CTAs of the first row tile
   long long out_step; int col_step;      // part number s of a sum cut in parts goes to out + s out_step, colsum + s col_step
   layer::Divisor by_Q, by_njt, by_tiles; // by_tiles: tiles of one part
-  const uint32_t* flags; int n_flags;    // work only if one of these is raised (null: always)
+  const uint32_t* flags; int n_flags;    // if given and none is raised: the sums are ready, `parts` of them, [parts][I][J to a multiple of 4]
+  const float* sums; int parts, vec;     // vec: rows of bias, res, out and pre start on 16 bytes
 };
 
 template <int BM, int BN> struct Cfg {
@@ -114,6 +115,67 @@ template <int W, bool B> struct Mover {
   }
 };
 
+// The epilogue of a tile whose sums are ready, in groups of four columns; the CTAs of a cluster take turns.
+template <int BN, int ACT> __device__ __noinline__ void finish_tile(const Args& p, long long i0, int j0, int X, int Y, int rank) {
+  constexpr int U = 4, PER = BN / 4;
+  const long long pitch = (p.J + 3) / 4 * 4, step = p.I * pitch;
+  const int j = j0 + (int)threadIdx.x % PER * 4, left = Y - (int)threadIdx.x % PER * 4;       // (NT is a multiple of PER: the same columns all the way)
+  if (left <= 0) return;
+  const bool vec = p.vec && left >= 4;
+  float bias[4] = {0.f, 0.f, 0.f, 0.f};
+  if (p.bias)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bias[e] = e < left ? p.bias[j + e] : 0.f;
+  const int hop = NT / PER * p.Q;
+#pragma unroll 1
+  for (int r0 = (int)threadIdx.x / PER + rank * (NT / PER); r0 < X; r0 += U * hop) {
+    float4 z[U], res[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * hop;
+      z[u] = res[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r >= X) continue;
+      const long long i = i0 + r;
+      z[u] = *reinterpret_cast<const float4*>(p.sums + i * pitch + j);
+      if (p.res) {
+        const float* s = p.res + i * p.ldr + j;
+        if (vec) res[u] = *reinterpret_cast<const float4*>(s);
+        else res[u] = make_float4(s[0], left > 1 ? s[1] : 0.f, left > 2 ? s[2] : 0.f, left > 3 ? s[3] : 0.f);
+      }
+    }
+    for (int k = 1; k < p.parts; ++k)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int r = r0 + u * hop;
+        if (r >= X) continue;
+        const float4 o = *reinterpret_cast<const float4*>(p.sums + k * step + (i0 + r) * pitch + j);
+        z[u].x += o.x; z[u].y += o.y; z[u].z += o.z; z[u].w += o.w;
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * hop;
+      if (r >= X) continue;
+      const long long i = i0 + r;
+      const float v[4] = {z[u].x + bias[0], z[u].y + bias[1], z[u].z + bias[2], z[u].w + bias[3]};
+      const float y[4] = {layer::act_value<ACT>(v[0]) + res[u].x, layer::act_value<ACT>(v[1]) + res[u].y, layer::act_value<ACT>(v[2]) + res[u].z,
+                          layer::act_value<ACT>(v[3]) + res[u].w};
+      float* out = p.out + i * p.ldo + j;
+      float* pre = p.pre ? p.pre + i * p.ldp + j : nullptr;
+      if (vec) {
+        if (pre) *reinterpret_cast<float4*>(pre) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4*>(out) = make_float4(y[0], y[1], y[2], y[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < left) {
+            if (pre) pre[e] = v[e];
+            out[e] = y[e];
+          }
+      }
+    }
+  }
+}
+
 template <int BM, int BN, int ACT>
 __global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Args p) {
   using C = Cfg<BM, BN>;
@@ -126,9 +188,11 @@ __global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Args
   const int j0 = (int)(tile - it * p.by_njt.d) * BN;
   const int kb0 = ((int)part * p.Q + rank) * p.kb_per, nkb = min(p.kb_per, p.n_kb - kb0);
   grid_dependency_sync();
-  if (p.flags && !split3::any_flag(p.flags, p.n_flags)) return;    // (the whole grid alike)
-
   const int X = (int)min((long long)BM, p.I - i0), Y = min(BN, p.J - j0);
+  if (p.flags && !split3::any_flag(p.flags, p.n_flags)) {          // (the whole grid alike)
+    finish_tile<BN, ACT>(p, i0, j0, X, Y, rank);
+    return;
+  }
   const Mover<BM, false> ma(p.a, p.a_i, p.a_k, i0, X);
   const Mover<BN, true> mb(p.b, p.b_j, p.b_k, j0, Y);
   auto fetch = [&](int kb) {
