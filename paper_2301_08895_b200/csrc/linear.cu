@@ -393,13 +393,15 @@ int pack(const void* src, long long rows, long long cols, long long ld, void* ds
 
 // ------------------------------------------------------------------ fp32 products
 
+// clusters of q CTAs, two per SM, that the GPU runs at a time (one more takes another round: 72 clusters of four 150 us, pairs 126)
+const int CLUSTERS[9] = {0, 296, 148, 93, 71, 56, 45, 37, 33};
+
 struct FmaPlan { int bm, Q, splits, kb_per; size_t part_bytes; double t; };
 // 64 x 64 or 128 x 128 tiles, how many CTAs of a cluster share a tile's sum, and into how many parts that go through scratch it is cut
 // besides.  A block of 32 k takes a CTA that is alone on its SM 0.95 or 3.3 us, two of them together 1.7 or 5.8 us (4096^3: 54
 // TFLOP/s); a round of CTAs costs 3 to 5 us for filling and results, a microsecond more in clusters, parts their way through L2 and a
-// launch.  CLUSTERS: clusters of q CTAs, two per SM, that the GPU runs at a time (72 clusters of four 150 us, pairs 126).
+// launch.
 FmaPlan plan_fma(long long I, int J, int K, int most = 64) {
-  static const int CLUSTERS[9] = {0, 296, 148, 93, 71, 56, 45, 37, 33};
   FmaPlan best = {};
   double least = 1e300;
   const int n_kb = (K + fp32::BK - 1) / fp32::BK;
@@ -423,12 +425,42 @@ FmaPlan plan_fma(long long I, int J, int K, int most = 64) {
   }
   return best;
 }
-typedef void (*FmaFn)(const fp32::Args);
+// Two small products that run at a time, dx (rows x n_in, sums over n_out) and dw (n_in x n_out, sums over the rows, in as many parts as
+// find a place): one launch if all CTAs of both are on the GPU together.  On their own each leaves most of it idle, and a second kernel
+// behind the first costs about 4 us more than alone (1111 x 401 x 123: 26 us, together 19.5).
+bool plan_fma_pair(long long rows, int n_in, int n_out, FmaPlan* dx, FmaPlan* dw) {
+  constexpr int BM = 64;
+  const int kx = (n_out + fp32::BK - 1) / fp32::BK, kw = (int)((rows + fp32::BK - 1) / fp32::BK);
+  const long long tx = (rows + BM - 1) / BM * ((n_in + BM - 1) / BM), tw = (long long)((n_in + BM - 1) / BM) * ((n_out + BM - 1) / BM);
+  const long long Jp = (n_out + 3) / 4 * 4;
+  double least = dx->t + dw->t + 4.0;
+  bool together = false;
+  for (int q = 1; q <= 8 && tx + tw <= CLUSTERS[q]; ++q) {
+    const int room = (int)((CLUSTERS[q] - tx) / tw);
+    const int px = (kx + q - 1) / q, pw = (kw + room * q - 1) / (room * q), split = (kw + pw * q - 1) / (pw * q);
+    if ((q - 1) * px >= kx || (split * q - 1) * pw >= kw) continue;      // (a part would be empty)
+    const size_t bytes = split > 1 ? round256((size_t)split * (n_in * Jp + n_out) * 4) : 0;
+    const double t = (px > pw ? px : pw) * ((tx + tw * split) * q > PLAN_SMS - 12 ? 1.7 : 0.95) + 3.0 + (q > 1 ? 1.0 : 0.0) +
+                     (split > 1 ? 2.5 + (double)bytes * 2.0 / 6e6 : 0.0);
+    if (t < least) {
+      least = t;
+      together = true;
+      *dx = FmaPlan{BM, q, 1, px, 0, t};
+      *dw = FmaPlan{BM, q, split, pw, bytes, 0.0};
+    }
+  }
+  return together;
+}
+
+typedef void (*FmaFn)(const fp32::Pair);
 template <int BM> FmaFn fma_fn(int act) {
   return act == ABS_ACT_RELU ? (FmaFn)fp32::fma_kernel<BM, BM, ABS_ACT_RELU> : act == ABS_ACT_GELU ? (FmaFn)fp32::fma_kernel<BM, BM, ABS_ACT_GELU>
          : act == ABS_ACT_SILU ? (FmaFn)fp32::fma_kernel<BM, BM, ABS_ACT_SILU> : (FmaFn)fp32::fma_kernel<BM, BM, ABS_ACT_NONE>;
 }
-int fma_product(fp32::Args p, const FmaPlan& pl, long long I, int J, int K, int act, float* part, int sms, int device, cudaStream_t s) {
+// One fp32 product: its matrices, its plan and where its parts go.
+struct Fma { fp32::Args p; FmaPlan pl; int I, J, K, act; float* part; };
+
+int fma_products(std::initializer_list<Fma> products, int sms, int device, cudaStream_t s) {
   static std::atomic<uint64_t> ready;
   cudaError_t e = cudaSuccess;
   if (!(ready.load(std::memory_order_acquire) >> device & 1)) {
@@ -439,37 +471,53 @@ int fma_product(fp32::Args p, const FmaPlan& pl, long long I, int J, int K, int 
     if (e != cudaSuccess) return fail(ABS_ECUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     ready.fetch_or(1ull << device, std::memory_order_release);
   }
-  for (long long pitch : {p.a_i, p.a_k, p.b_k, p.b_j})
-    if (pitch > (1ll << 24)) return fail(ABS_EUNSUPPORTED, "fp32: row pitch %lld above 2^24", pitch);
-  p.I = (int)I; p.J = J; p.K = K;
-  p.n_kb = (K + fp32::BK - 1) / fp32::BK;
-  p.n_jt = (J + pl.bm - 1) / pl.bm;
-  p.Q = pl.Q; p.kb_per = pl.kb_per;
-  p.by_Q = Divisor((uint32_t)pl.Q);
-  p.by_njt = Divisor((uint32_t)p.n_jt);
-  const long long tiles = (I + pl.bm - 1) / pl.bm * p.n_jt, ctas = tiles * pl.splits * pl.Q;
-  const fp32::Args whole = p;
-  if (pl.splits > 1) {
-    p.bias = p.res = nullptr;
-    p.pre = nullptr;
-    p.ldo = (J + 3) / 4 * 4;
-    p.out = part;
-    p.out_step = I * p.ldo;
-    p.col_step = J;
-    if (p.colsum) p.colsum = part + pl.splits * p.out_step;
+  fp32::Pair pair = {};
+  long long ctas = 0;
+  int n = 0;
+  for (const Fma& f : products) {
+    const FmaPlan& pl = f.pl;
+    fp32::Args& p = pair.a[n++];
+    p = f.p;
+    p.I = f.I; p.J = f.J; p.K = f.K;
+    p.n_kb = (f.K + fp32::BK - 1) / fp32::BK;
+    p.n_jt = (f.J + pl.bm - 1) / pl.bm;
+    p.Q = pl.Q; p.kb_per = pl.kb_per;
+    p.by_Q = Divisor((uint32_t)pl.Q);
+    p.by_njt = Divisor((uint32_t)p.n_jt);
+    const long long tiles = ((long long)f.I + pl.bm - 1) / pl.bm * p.n_jt;
+    if (pl.splits > 1) {
+      p.bias = p.res = nullptr;
+      p.pre = nullptr;
+      p.ldo = (f.J + 3) / 4 * 4;
+      p.out = f.part;
+      p.out_step = f.I * p.ldo;
+      p.col_step = f.J;
+      if (p.colsum) p.colsum = f.part + pl.splits * p.out_step;
+    }
+    p.by_tiles = Divisor((uint32_t)(tiles < 0x7fffffff ? tiles : 1));
+    ctas += tiles * pl.splits * pl.Q;
+    if (ctas > 0x7fffffff) return fail(ABS_EUNSUPPORTED, "%lld tiles in one product", ctas);
+    if (n == 1) pair.first = (uint32_t)ctas;
   }
-  p.by_tiles = Divisor((uint32_t)(tiles < 0x7fffffff ? tiles : 1));
-  if (ctas > 0x7fffffff) return fail(ABS_EUNSUPPORTED, "%lld tiles in one product", ctas);
-  const int in_kernel = pl.splits > 1 ? ABS_ACT_NONE : act;
-  e = pl.bm == 64 ? launch(fma_fn<64>(in_kernel), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<64, 64>::SMEM, pl.Q, s, p)
-                  : launch(fma_fn<128>(in_kernel), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<128, 128>::SMEM, pl.Q, s, p);
-  if (e == cudaSuccess && pl.splits > 1) {
-    const Result r = {whole.bias, whole.res, whole.ldr, whole.out, whole.ldo, whole.pre, whole.ldp, act};
-    e = finish<float>(part, pl.splits, (int)I, J, r, sms, s);
-    if (e == cudaSuccess && whole.colsum)
-      e = launch(column_kernel<float>, dim3((unsigned)((J + 31) / 32)), 256, 0, 1, s, (const float*)p.colsum, pl.splits, J, (void*)whole.colsum);
+  const Fma& one = *products.begin();                    // (two products have one tile, one cluster and no activation)
+  const int in_kernel = one.pl.splits > 1 ? ABS_ACT_NONE : one.act;
+  e = one.pl.bm == 64 ? launch(fma_fn<64>(in_kernel), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<64, 64>::SMEM, one.pl.Q, s, pair)
+                      : launch(fma_fn<128>(in_kernel), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<128, 128>::SMEM, one.pl.Q, s, pair);
+  n = 0;
+  for (const Fma& f : products) {
+    const float* sums = pair.a[n++].colsum;
+    if (e != cudaSuccess || f.pl.splits == 1) continue;
+    const Result r = {f.p.bias, f.p.res, f.p.ldr, f.p.out, f.p.ldo, f.p.pre, f.p.ldp, f.act};
+    e = finish<float>(f.part, f.pl.splits, f.I, f.J, r, sms, s);
+    if (e == cudaSuccess && sums)
+      e = launch(column_kernel<float>, dim3((unsigned)((f.J + 31) / 32)), 256, 0, 1, s, sums, f.pl.splits, f.J, (void*)f.p.colsum);
   }
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
+}
+int check_pitches(std::initializer_list<long long> pitches) {
+  for (long long pitch : pitches)
+    if (pitch > (1ll << 24)) return fail(ABS_EUNSUPPORTED, "fp32: row pitch %lld above 2^24", pitch);
+  return ABS_OK;
 }
 
 // ------------------------------------------------------------------ fp32 products on the tensor cores
@@ -517,7 +565,7 @@ int pieces_product(const split3::Matrix& a, int a_mn, const split3::Matrix& b, i
   plain.sums = part; plain.parts = pl.splits;
   auto whole = [](const void* p, long long ld) { return !p || ((uintptr_t)p % 16 == 0 && ld % 4 == 0); };
   plain.vec = whole(plain.res, plain.ldr) && whole(plain.out, plain.ldo) && whole(plain.pre, plain.ldp);
-  return fma_product(plain, plan_fma(I, J, K, 1), I, J, K, act, nullptr, sms, device, s);
+  return fma_products({{plain, plan_fma(I, J, K, 1), I, J, K, act, nullptr}}, sms, device, s);
 }
 
 // ------------------------------------------------------------------ few rows, few outputs
@@ -611,7 +659,7 @@ FwdPlan fwd_plan(long long rows, int n_in, int n_out, int dtype, bool pack_x, bo
   f.total = f.part + f.tc.part_bytes;
   return f;
 }
-struct GradPlan { size_t dz, sums, x, w, part, total; long long ld_dz; int chunk, chunks; FmaPlan dx, dw; Plan tx, tw; bool pieces; size_t pz, px, pw, flags; };
+struct GradPlan { size_t dz, sums, x, w, part, total; long long ld_dz; int chunk, chunks; FmaPlan dx, dw, dx2, dw2; Plan tx, tw; bool together, pieces; size_t pz, px, pw, flags; };
 GradPlan grad_plan(long long rows, int n_in, int n_out, int dtype, bool need_dz, bool pack_x, bool pack_w) {
   GradPlan g = {};
   const size_t esz = dtype == ABS_FP32 ? 4 : 2;
@@ -629,12 +677,14 @@ GradPlan grad_plan(long long rows, int n_in, int n_out, int dtype, bool need_dz,
   size_t a, b;
   if (dtype == ABS_FP32) {
     g.dx = plan_fma(rows, n_in, n_out); g.dw = plan_fma(n_in, n_out, (int)rows);
-    a = g.dx.part_bytes; b = g.dw.part_bytes;
+    g.dx2 = g.dx; g.dw2 = g.dw;
+    g.together = plan_fma_pair(rows, n_in, n_out, &g.dx2, &g.dw2);
+    a = g.dx.part_bytes; b = g.dw.part_bytes > g.dw2.part_bytes ? g.dw.part_bytes : g.dw2.part_bytes;
     g.tx = plan_pieces(rows, n_in, n_out);
     g.tw = plan_pieces(n_in, n_out, rows);
     const size_t bz = piece_bytes(rows, n_out), bx = piece_bytes(rows, n_in), bw = piece_bytes(n_in, n_out);
     g.pieces = pieces_fit(rows, n_in, g.tx, bz + bx + bw) && pieces_fit(n_in, n_out, g.tw, 0) &&
-               g.tx.t + g.tw.t + split_time(bz + bx + bw) < g.dx.t + g.dw.t;
+               g.tx.t + g.tw.t + split_time(bz + bx + bw) < (g.together ? g.dx2.t : g.dx.t + g.dw.t);
     if (g.pieces) {
       g.pz = g.part; g.px = g.pz + bz; g.pw = g.px + bx;
       g.flags = g.pw + bw;
@@ -689,6 +739,7 @@ extern "C" int abs_linear(const void* x, long long ldx, const void* w, long long
   const bool pack_x = bf16 && !tma_able(x, rows, ldx), pack_w = bf16 && !tma_able(w, n_in, ldw);
   const bool narrow = !few && bf16 && !pack_x && few_outputs_size(rows, n_in, n_out);
   const FwdPlan f = few || narrow ? FwdPlan{} : fwd_plan(rows, n_in, n_out, dtype, pack_x, pack_w);
+  if (!bf16 && !few && (rc = check_pitches({ldx, ldw})) != ABS_OK) return rc;
   if ((rc = check_scratch(scratch, scratch_bytes, f.total, {sx, sw, sb, sr, sy, sp})) != ABS_OK) return rc;
   cudaStream_t s = (cudaStream_t)stream;
   int device, sms;
@@ -710,7 +761,7 @@ extern "C" int abs_linear(const void* x, long long ldx, const void* w, long long
       if (e != cudaSuccess) return fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
       return pieces_product(mx, 0, mw, 1, p, f.tc, (int)rows, n_out, n_in, act, flags, (float*)(sc + f.part), sms, device, s);
     }
-    return fma_product(p, f.fma, rows, n_out, n_in, act, (float*)scratch, sms, device, s);
+    return fma_products({{p, f.fma, (int)rows, n_out, n_in, act, (float*)scratch}}, sms, device, s);
   }
   char* sc = (char*)scratch;
   Operand a = {x, rows, n_in, tma_pitch(rows, n_in, ldx)}, b = {w, n_in, n_out, tma_pitch(n_in, n_out, ldw)};
@@ -762,12 +813,13 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
   const bool need_dz = act != ABS_ACT_NONE || (bf16 && (dx || dw) && !tma_able(dy, rows, lddy));
   const bool pack_x = bf16 && dw && !tma_able(x, rows, ldx), pack_w = bf16 && dx && !tma_able(w, n_in, ldw);
   const GradPlan g = grad_plan(rows, n_in, n_out, dtype, need_dz, pack_x, pack_w);
+  const long long lddz = need_dz ? g.ld_dz : lddy;
+  if (!bf16 && (rc = check_pitches({dx || dw ? lddz : 0, dw ? ldx : 0, dx ? ldw : 0})) != ABS_OK) return rc;
   if ((rc = check_scratch(scratch, scratch_bytes, g.total, {ins[0], ins[1], ins[2], ins[3], outs[0], outs[1], outs[2]})) != ABS_OK) return rc;
   int device, sms;
   if ((rc = current_device(&device, &sms)) != ABS_OK) return rc;
   char* sc = (char*)scratch;
   const void* dz = need_dz ? sc + g.dz : dy;
-  const long long lddz = need_dz ? g.ld_dz : lddy;
   const bool with_dw = !bf16 && !g.pieces && dw && db; // the column sums come with the product
   float* part = db && !with_dw ? (float*)(sc + g.sums) : nullptr;
   cudaError_t e = cudaSuccess;
@@ -794,25 +846,23 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
       e = dx && dw ? split({mz, mx, mw}, &flags, s) : dw ? split({mz, mx}, &flags, s) : split({mz, mw}, &flags, s);
       if (e != cudaSuccess) return fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
     }
-    if (dx) {
-      fp32::Args p = {};
-      p.a = (const float*)dz; p.a_i = lddz; p.a_k = 1;
-      p.b = (const float*)w; p.b_k = 1; p.b_j = ldw;
-      p.out = (float*)dx; p.ldo = lddx;
-      if (g.pieces) rc = pieces_product(mz, 0, mw, 0, p, g.tx, (int)rows, n_in, n_out, ABS_ACT_NONE, flags, (float*)(sc + g.part), sms, device, s);
-      else rc = fma_product(p, g.dx, rows, n_in, n_out, ABS_ACT_NONE, (float*)(sc + g.part), sms, device, s);
-      if (rc != ABS_OK) return rc;
+    fp32::Args px = {}, pw = {};
+    px.a = (const float*)dz; px.a_i = lddz; px.a_k = 1;
+    px.b = (const float*)w; px.b_k = 1; px.b_j = ldw;
+    px.out = (float*)dx; px.ldo = lddx;
+    pw.a = (const float*)x; pw.a_i = 1; pw.a_k = ldx;
+    pw.b = (const float*)dz; pw.b_k = lddz; pw.b_j = 1;
+    pw.out = (float*)dw; pw.ldo = lddw;
+    pw.colsum = with_dw ? (float*)db : nullptr;
+    float* sums = (float*)(sc + g.part);
+    if (g.pieces) {
+      if (dx && (rc = pieces_product(mz, 0, mw, 0, px, g.tx, (int)rows, n_in, n_out, ABS_ACT_NONE, flags, sums, sms, device, s)) != ABS_OK) return rc;
+      return dw ? pieces_product(mx, 1, mz, 1, pw, g.tw, n_in, n_out, (int)rows, ABS_ACT_NONE, flags, sums, sms, device, s) : ABS_OK;
     }
-    if (dw) {
-      fp32::Args p = {};
-      p.a = (const float*)x; p.a_i = 1; p.a_k = ldx;
-      p.b = (const float*)dz; p.b_k = lddz; p.b_j = 1;
-      p.out = (float*)dw; p.ldo = lddw;
-      p.colsum = with_dw ? (float*)db : nullptr;
-      if (g.pieces) rc = pieces_product(mx, 1, mz, 1, p, g.tw, n_in, n_out, (int)rows, ABS_ACT_NONE, flags, (float*)(sc + g.part), sms, device, s);
-      else rc = fma_product(p, g.dw, n_in, n_out, (int)rows, ABS_ACT_NONE, (float*)(sc + g.part), sms, device, s);
-      if (rc != ABS_OK) return rc;
-    }
+    if (dx && dw && g.together)
+      return fma_products({{px, g.dx2, (int)rows, n_in, n_out, ABS_ACT_NONE, nullptr}, {pw, g.dw2, n_in, n_out, (int)rows, ABS_ACT_NONE, sums}}, sms, device, s);
+    if (dx && (rc = fma_products({{px, g.dx, (int)rows, n_in, n_out, ABS_ACT_NONE, sums}}, sms, device, s)) != ABS_OK) return rc;
+    if (dw && (rc = fma_products({{pw, g.dw, n_in, n_out, (int)rows, ABS_ACT_NONE, sums}}, sms, device, s)) != ABS_OK) return rc;
     return ABS_OK;
   }
   const Operand od = {dz, rows, n_out, tma_pitch(rows, n_out, lddz)};

@@ -32,6 +32,8 @@ struct Args {
   const float* sums; int parts, vec;     // vec: rows of bias, res, out and pre start on 16 bytes
 };
 
+struct Pair { Args a[2]; uint32_t first; };          // CTAs of the first product; those behind them work on the second
+
 template <int BM, int BN> struct Cfg {
   static constexpr int LDA = BM + 4, LDB = BN + 4;       // (4 modulo 32; with the swizzle no bank is hit twice, or twice at most)
   static constexpr int STAGES = 3;
@@ -177,12 +179,15 @@ template <int BN, int ACT> __device__ __noinline__ void finish_tile(const Args& 
 }
 
 template <int BM, int BN, int ACT>
-__global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Args p) {
+__global__ void __launch_bounds__(NT, 2) fma_kernel(const __grid_constant__ Pair pair) {
   using C = Cfg<BM, BN>;
   constexpr int STAGES = C::STAGES, KG = C::KG, KPG = BK / KG, TX = BN / 8;
   extern __shared__ __align__(16) float sm[];
-  const uint32_t work = p.by_Q.div(blockIdx.x), part = p.out_step ? p.by_tiles.div(work) : 0u, tile = work - part * p.by_tiles.d;
-  const int rank = (int)(blockIdx.x - work * p.by_Q.d);
+  const bool second = blockIdx.x >= pair.first;
+  const Args& p = pair.a[second];
+  const uint32_t block = second ? blockIdx.x - pair.first : blockIdx.x;
+  const uint32_t work = p.by_Q.div(block), part = p.out_step ? p.by_tiles.div(work) : 0u, tile = work - part * p.by_tiles.d;
+  const int rank = (int)(block - work * p.by_Q.d);
   const uint32_t it = p.by_njt.div(tile);
   const long long i0 = (long long)it * BM;
   const int j0 = (int)(tile - it * p.by_njt.d) * BN;
