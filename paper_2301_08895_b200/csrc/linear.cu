@@ -393,10 +393,11 @@ int pack(const void* src, long long rows, long long cols, long long ld, void* ds
 
 // ------------------------------------------------------------------ fp32 products
 
-// clusters of q CTAs, two per SM, that the GPU runs at a time (one more takes another round: 72 clusters of four 150 us, pairs 126)
-const int CLUSTERS[9] = {0, 296, 148, 93, 71, 56, 45, 37, 33};
+// clusters of q CTAs that the GPU runs at a time, as the driver's occupancy query tells, with two CTAs per SM (72 clusters of four ran in two
+// rounds, 150 us, pairs 126) and with one
+const int CLUSTERS[9] = {0, 296, 148, 93, 71, 56, 45, 37, 33}, ALONE[9] = {0, 148, 74, 45, 33, 26, 22, 15, 15};
 
-struct FmaPlan { int bm, Q, splits, kb_per; size_t part_bytes; double t; };
+struct FmaPlan { int bm, Q, splits, kb_per; size_t part_bytes; double t; bool alone; };    // alone: one CTA per SM, by its shared memory
 // 64 x 64 or 128 x 128 tiles, how many CTAs of a cluster share a tile's sum, and into how many parts that go through scratch it is cut
 // besides.  A block of 32 k takes a CTA that is alone on its SM 0.95 or 3.3 us, two of them together 1.7 or 5.8 us (4096^3: 54
 // TFLOP/s); a round of CTAs costs 3 to 5 us for filling and results, a microsecond more in clusters, parts their way through L2 and a
@@ -417,9 +418,10 @@ FmaPlan plan_fma(long long I, int J, int K, int most = 64) {
         if ((long long)(chunks - 1) * per >= n_kb) continue;     // (a part would be empty)
         const long long n = tiles * split, full = n / CLUSTERS[q], rest = n - full * CLUSTERS[q];
         const double around = (bm == 64 ? 3.0 : 5.0) + (q > 1 ? 1.0 : 0.0);
-        const double last = rest == 0 ? 0.0 : (rest * q > PLAN_SMS - 12 ? two : one) * per + around;
+        const bool alone = full == 0 && rest <= ALONE[q], apart = alone || (q == 1 && rest <= ALONE[1]);
+        const double last = rest == 0 ? 0.0 : (apart ? one : two) * per + around;
         const double t = (double)full * (two * per + around) + last + (split > 1 ? 2.5 + (double)bytes * 2.0 / 6e6 : 0.0);
-        if (t < least) { least = t; best = FmaPlan{bm, q, split, per, bytes, t}; }
+        if (t < least) { least = t; best = FmaPlan{bm, q, split, per, bytes, t, alone}; }
       }
     }
   }
@@ -440,13 +442,14 @@ bool plan_fma_pair(long long rows, int n_in, int n_out, FmaPlan* dx, FmaPlan* dw
     const int px = (kx + q - 1) / q, pw = (kw + room * q - 1) / (room * q), split = (kw + pw * q - 1) / (pw * q);
     if ((q - 1) * px >= kx || (split * q - 1) * pw >= kw) continue;      // (a part would be empty)
     const size_t bytes = split > 1 ? round256((size_t)split * (n_in * Jp + n_out) * 4) : 0;
-    const double t = (px > pw ? px : pw) * ((tx + tw * split) * q > PLAN_SMS - 12 ? 1.7 : 0.95) + 3.0 + (q > 1 ? 1.0 : 0.0) +
+    const bool alone = tx + tw * split <= ALONE[q];
+    const double t = (px > pw ? px : pw) * (alone ? 0.95 : 1.7) + 3.0 + (q > 1 ? 1.0 : 0.0) +
                      (split > 1 ? 2.5 + (double)bytes * 2.0 / 6e6 : 0.0);
     if (t < least) {
       least = t;
       together = true;
-      *dx = FmaPlan{BM, q, 1, px, 0, t};
-      *dw = FmaPlan{BM, q, split, pw, bytes, 0.0};
+      *dx = FmaPlan{BM, q, 1, px, 0, t, alone};
+      *dw = FmaPlan{BM, q, split, pw, bytes, 0.0, alone};
     }
   }
   return together;
@@ -460,13 +463,18 @@ template <int BM> FmaFn fma_fn(int act) {
 // One fp32 product: its matrices, its plan and where its parts go.
 struct Fma { fp32::Args p; FmaPlan pl; int I, J, K, act; float* part; };
 
+// More than half of an SM's shared memory: CTAs of a cluster otherwise share SMs while others idle (1000 x 784 x 128 on 128 CTAs: 15.9 us in
+// pairs, 12.9 alone).
+constexpr size_t ALONE_SMEM = 120 * 1024;
+static_assert(ALONE_SMEM >= fp32::Cfg<64, 64>::SMEM && ALONE_SMEM >= fp32::Cfg<128, 128>::SMEM, "");
+
 int fma_products(std::initializer_list<Fma> products, int sms, int device, cudaStream_t s) {
   static std::atomic<uint64_t> ready;
   cudaError_t e = cudaSuccess;
   if (!(ready.load(std::memory_order_acquire) >> device & 1)) {
     for (int i = ABS_ACT_NONE; i <= ABS_ACT_SILU && e == cudaSuccess; ++i) {
-      e = allow_smem(fma_fn<64>(i), fp32::Cfg<64, 64>::SMEM);
-      if (e == cudaSuccess) e = allow_smem(fma_fn<128>(i), fp32::Cfg<128, 128>::SMEM);
+      e = allow_smem(fma_fn<64>(i), ALONE_SMEM);
+      if (e == cudaSuccess) e = allow_smem(fma_fn<128>(i), ALONE_SMEM);
     }
     if (e != cudaSuccess) return fail(ABS_ECUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     ready.fetch_or(1ull << device, std::memory_order_release);
@@ -501,8 +509,8 @@ int fma_products(std::initializer_list<Fma> products, int sms, int device, cudaS
   }
   const Fma& one = *products.begin();                    // (two products have one tile, one cluster and no activation)
   const int in_kernel = one.pl.splits > 1 ? ABS_ACT_NONE : one.act;
-  e = one.pl.bm == 64 ? launch(fma_fn<64>(in_kernel), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<64, 64>::SMEM, one.pl.Q, s, pair)
-                      : launch(fma_fn<128>(in_kernel), dim3((unsigned)ctas), fp32::NT, fp32::Cfg<128, 128>::SMEM, one.pl.Q, s, pair);
+  const size_t smem = one.pl.alone ? ALONE_SMEM : one.pl.bm == 64 ? fp32::Cfg<64, 64>::SMEM : fp32::Cfg<128, 128>::SMEM;
+  e = launch(one.pl.bm == 64 ? fma_fn<64>(in_kernel) : fma_fn<128>(in_kernel), dim3((unsigned)ctas), fp32::NT, smem, one.pl.Q, s, pair);
   n = 0;
   for (const Fma& f : products) {
     const float* sums = pair.a[n++].colsum;
@@ -526,6 +534,10 @@ constexpr int SPLIT_BLOCKS = 4 * PLAN_SMS;
 constexpr size_t FLAG_BYTES = (SPLIT_BLOCKS * 4 + 255) / 256 * 256;
 long long rows64(long long rows) { return (rows + 63) / 64 * 64; }
 size_t piece_bytes(long long rows, int cols) { return round256((size_t)rows64(rows) * ((cols + 7) / 8 * 8) * 6); }
+// The pieces' way is taken where its time by the models is less; plan_fma leaves out what every launch costs.  Around the border, us as plain
+// fused multiply-adds and in pieces: 256 x 512 x 512 11.0, 13.3; 1000 x 784 x 128 12.8, 15.9; 400 x 1024 x 512 24.0, 17.0; 20000 x 128 x 128
+// 32.6, 27.2; 1024 x 785 x 512 32.2, 20.2; gradients of 512 x 512 x 512 22.5, 28.2, of 1024 x 512 x 512 45.6, 34.0.
+constexpr double PLAIN_START = 3.0;
 double split_time(size_t bytes) { return 3.0 + (double)bytes * (10.0 / 6.0) / 4e6; }
 // matrices whose pieces and results stay well inside scratch and the copies' coordinates
 bool pieces_fit(long long I, int J, const Plan& pl, size_t bytes) {
@@ -644,7 +656,7 @@ FwdPlan fwd_plan(long long rows, int n_in, int n_out, int dtype, bool pack_x, bo
     f.total = f.fma.part_bytes;
     f.tc = plan_pieces(rows, n_out, n_in);
     const size_t bx = piece_bytes(rows, n_in), bw = piece_bytes(n_in, n_out);
-    f.pieces = pieces_fit(rows, n_out, f.tc, bx + bw) && f.tc.t + split_time(bx + bw) < f.fma.t;
+    f.pieces = pieces_fit(rows, n_out, f.tc, bx + bw) && f.tc.t + split_time(bx + bw) < f.fma.t + PLAIN_START;
     if (f.pieces) {
       f.w = bx;
       f.part = bx + bw;
@@ -684,7 +696,7 @@ GradPlan grad_plan(long long rows, int n_in, int n_out, int dtype, bool need_dz,
     g.tw = plan_pieces(n_in, n_out, rows);
     const size_t bz = piece_bytes(rows, n_out), bx = piece_bytes(rows, n_in), bw = piece_bytes(n_in, n_out);
     g.pieces = pieces_fit(rows, n_in, g.tx, bz + bx + bw) && pieces_fit(n_in, n_out, g.tw, 0) &&
-               g.tx.t + g.tw.t + split_time(bz + bx + bw) < (g.together ? g.dx2.t : g.dx.t + g.dw.t);
+               g.tx.t + g.tw.t + split_time(bz + bx + bw) < (g.together ? g.dx2.t : g.dx.t + g.dw.t) + PLAIN_START;
     if (g.pieces) {
       g.pz = g.part; g.px = g.pz + bz; g.pw = g.px + bx;
       g.flags = g.pw + bw;

@@ -29,7 +29,7 @@ struct Args {
   long long out_step; int col_step;      // part number s of a sum cut in parts goes to out + s out_step, colsum + s col_step
   layer::Divisor by_Q, by_njt, by_tiles; // by_tiles: tiles of one part
   const uint32_t* flags; int n_flags;    // if given and none is raised: the sums are ready, `parts` of them, [parts][I][J to a multiple of 4]
-  const float* sums; int parts, vec;     // vec: rows of bias, res, out and pre start on 16 bytes
+  const float* sums; int parts, vec;     // vec: rows of res, out and pre start on 16 bytes
 };
 
 struct Pair { Args a[2]; uint32_t first; };          // CTAs of the first product; those behind them work on the second

@@ -4,9 +4,12 @@
 //   operand     dX[m][k] = sum_n dZ[m][n] W[k][n]                             both: n contiguous
 //   weights     dW[k][n] = sum_m X[m][k] dZ[m][n]                             neither: the sum runs over rows
 //
-// (and in fp32 as six passes over three pieces of each operand, see linear_split.cuh) are one kernel: C[i][j] = sum_t A(i, t) B(j, t), each operand either with t contiguous ("K-major": one box of 64 t per
+// are one kernel: C[i][j] = sum_t A(i, t) B(j, t), each operand either with t contiguous ("K-major": one box of 64 t per
 // 128 rows) or with i (j) contiguous ("MN-major": boxes of 64 columns x 64 t).  Both arrive by TMA in the 128-byte swizzle
 // that tcgen05.mma reads; sizes that do not fill a tile are filled with zeros by the copies and clipped by the stores.
+//
+// Products of fp32 matrices come here as three bf16 pieces of each (linear_split.cuh): the sum runs over six pairs of pieces, which lie
+// a_step and b_step rows apart.
 //
 // Persistent and warp-specialised: warp 0 issues the copies of a ring of stages, warp 1 the products into two alternating
 // accumulators in tensor memory, warps 2..9 take the other accumulator through the epilogue meanwhile: registers, a box of 32
@@ -179,7 +182,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
       for (int t = unit; t < p.n_tiles && ok; t += n_units) {
         const Tile c = tile_of(t);
         const int j0 = c.j0 + rank * BH;
-        int pass = c.kb0 / p.kb_pass, k0 = (c.kb0 - pass * p.kb_pass) * BK;
+        int pass = c.kb0 / p.kb_pass, at = c.kb0 - pass * p.kb_pass;
         int ra = p.a_step * (int)(split3::A_PIECE >> 4 * pass & 15u), rb = p.b_step * (int)(split3::B_PIECE >> 4 * pass & 15u);
         for (int kb = 0; kb < c.n_kb; ++kb) {
           if (!mbar_wait(&empty[stage], phase ^ 1u, abort)) { ok = false; break; }
@@ -189,6 +192,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             mbar_expect_tx(&full[stage], CG * C::STAGE_BYTES);
             armed[stage] = (int)phase;
           }
+          const int k0 = at * BK;
           if (p.a_mn) {
             for (int j = 0; j < BM / 64; ++j) load(sa + j * 8192, &map_a, stage, c.i0 + 64 * j, k0 + ra);
           } else {
@@ -199,9 +203,8 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
           } else {
             load(sb, &map_b, stage, k0, j0 + rb);
           }
-          k0 += BK;
-          if (k0 == p.kb_pass * BK) {
-            k0 = 0;
+          if (++at == p.kb_pass) {
+            at = 0;
             ++pass;
             ra = p.a_step * (int)(split3::A_PIECE >> 4 * pass & 15u);
             rb = p.b_step * (int)(split3::B_PIECE >> 4 * pass & 15u);
