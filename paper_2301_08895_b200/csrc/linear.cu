@@ -314,11 +314,11 @@ bool tma_able(const void* p, long long rows, long long ld) { return (uintptr_t)p
 long long tma_pitch(long long rows, long long cols, long long ld) { return rows == 1 ? (cols + 7) / 8 * 8 : ld; }
 size_t pack_bytes(long long rows, long long cols) { return round256((size_t)rows * ((cols + 7) / 8 * 8) * 2); }
 
-template <int BN, int CG>
+template <int BN, int CG, bool PIECES>
 cudaError_t launch_dense(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const CUtensorMap& z, const dense::Args& p, int sms, int device,
                          cudaStream_t s) {
   static std::atomic<uint64_t> ready;
-  auto* kernel = dense::dense_kernel<BN, CG>;
+  auto* kernel = dense::dense_kernel<BN, CG, PIECES>;
   if (!(ready.load(std::memory_order_acquire) >> device & 1)) {
     const cudaError_t e = allow_smem(kernel, dense::Cfg<BN, CG>::SMEM_BYTES);
     if (e != cudaSuccess) return e;
@@ -326,6 +326,14 @@ cudaError_t launch_dense(const CUtensorMap& a, const CUtensorMap& b, const CUten
   }
   const int units = sms / CG < p.n_tiles ? sms / CG : p.n_tiles;
   return launch(kernel, dim3((unsigned)(units * CG)), dense::THREADS, dense::Cfg<BN, CG>::SMEM_BYTES, CG, s, a, b, o, z, p);
+}
+
+template <bool PIECES>
+cudaError_t launch_tile(const Plan& pl, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const CUtensorMap& z, const dense::Args& p, int sms,
+                        int device, cudaStream_t s) {
+  if (pl.cg == 2) return pl.bn == 256 ? launch_dense<256, 2, PIECES>(a, b, o, z, p, sms, device, s) : launch_dense<128, 2, PIECES>(a, b, o, z, p, sms, device, s);
+  return pl.bn == 256 ? launch_dense<256, 1, PIECES>(a, b, o, z, p, sms, device, s)
+         : pl.bn == 128 ? launch_dense<128, 1, PIECES>(a, b, o, z, p, sms, device, s) : launch_dense<64, 1, PIECES>(a, b, o, z, p, sms, device, s);
 }
 
 __device__ int g_status;                 // set by a kernel whose bounded wait ran out; read and cleared by abs_op_status
@@ -377,8 +385,8 @@ int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, in
   mz = mo;
   if (p.pre_tma) ok = ok && matrix_map(&mz, r.pre, I, J, tma_pitch(I, J, r.ldp), 32);
   if (!ok) return fail(ABS_ECUDA, "cuTensorMapEncodeTiled failed");
-  cudaError_t e = pl.cg == 2 ? (pl.bn == 256 ? launch_dense<256, 2>(ma, mb, mo, mz, p, sms, device, s) : launch_dense<128, 2>(ma, mb, mo, mz, p, sms, device, s)) : pl.bn == 256 ? launch_dense<256, 1>(ma, mb, mo, mz, p, sms, device, s)
-                  : pl.bn == 128 ? launch_dense<128, 1>(ma, mb, mo, mz, p, sms, device, s) : launch_dense<64, 1>(ma, mb, mo, mz, p, sms, device, s);
+  auto* go = pieces ? &launch_tile<true> : &launch_tile<false>;
+  cudaError_t e = go(pl, ma, mb, mo, mz, p, sms, device, s);
   if (e == cudaSuccess && pl.splits > 1 && !pieces) e = finish<__nv_bfloat16>(part, pl.splits, I, J, r, sms, s);
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }

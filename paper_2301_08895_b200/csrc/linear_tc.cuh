@@ -105,7 +105,8 @@ __device__ __forceinline__ void box_rows_out(const uint8_t* box, int lane, __nv_
   }
 }
 
-template <int BN, int CG>
+// PIECES: fp32 operands in pieces, partial results; an own instance, since the passes' bookkeeping costs the bf16 products 3 % (205 us for 199).
+template <int BN, int CG, bool PIECES>
 __global__ void __launch_bounds__(THREADS, 1)
 dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
              const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_pre, const __grid_constant__ Args p) {
@@ -182,8 +183,16 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
       for (int t = unit; t < p.n_tiles && ok; t += n_units) {
         const Tile c = tile_of(t);
         const int j0 = c.j0 + rank * BH;
-        int pass = c.kb0 / p.kb_pass, at = c.kb0 - pass * p.kb_pass;
-        int ra = p.a_step * (int)(split3::A_PIECE >> 4 * pass & 15u), rb = p.b_step * (int)(split3::B_PIECE >> 4 * pass & 15u);
+        int pass = 0, at = c.kb0, ra = 0, rb = 0;      // pair of pieces, block in its pass, rows to the pieces
+        auto pieces = [&] {
+          ra = p.a_step * (int)(split3::A_PIECE >> 4 * pass & 15u);
+          rb = p.b_step * (int)(split3::B_PIECE >> 4 * pass & 15u);
+        };
+        if (PIECES) {
+          pass = at / p.kb_pass;
+          at -= pass * p.kb_pass;
+          pieces();
+        }
         for (int kb = 0; kb < c.n_kb; ++kb) {
           if (!mbar_wait(&empty[stage], phase ^ 1u, abort)) { ok = false; break; }
           uint8_t* sa = smem + (size_t)stage * C::STAGE_BYTES;
@@ -192,7 +201,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             mbar_expect_tx(&full[stage], CG * C::STAGE_BYTES);
             armed[stage] = (int)phase;
           }
-          const int k0 = at * BK;
+          const int k0 = PIECES ? at * BK : (c.kb0 + kb) * BK;
           if (p.a_mn) {
             for (int j = 0; j < BM / 64; ++j) load(sa + j * 8192, &map_a, stage, c.i0 + 64 * j, k0 + ra);
           } else {
@@ -203,11 +212,10 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
           } else {
             load(sb, &map_b, stage, k0, j0 + rb);
           }
-          if (++at == p.kb_pass) {
+          if (PIECES && ++at == p.kb_pass) {
             at = 0;
             ++pass;
-            ra = p.a_step * (int)(split3::A_PIECE >> 4 * pass & 15u);
-            rb = p.b_step * (int)(split3::B_PIECE >> 4 * pass & 15u);
+            pieces();
           }
           if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
         }
@@ -280,7 +288,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
       tc_fence_after();
       const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN);
       if (works && row0 < p.I) {               // (uniform in the warp)
-        if (p.partial) {
+        if (PIECES || p.partial) {
 #pragma unroll 1
           for (int c0 = half * HALF_COLS; c0 < (half + 1) * HALF_COLS && c.j0 + c0 < p.J; c0 += 32) {
             uint32_t v[32];
