@@ -951,7 +951,7 @@ Plan plan(long long samples, long long positions, int C, int G, int dtype, bool 
   Plan p = {};
   const int D = C / G;
   const size_t esz = dtype == ABS_FP32 ? 4 : 2;
-  const int VE = vec ? (int)(16 / esz) : 1;
+  const int VE = vec && (size_t)C * esz % 16 == 0 ? (int)(16 / esz) : 1;      // (a position of fewer channels, or a part more, has no whole vectors)
   int unit = 1;                          // groups that make whole vectors
   while ((long long)unit * D % VE) ++unit;
   const double sample_bytes = (double)positions * C * esz * (grad ? 2 : 1);

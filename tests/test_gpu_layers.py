@@ -835,6 +835,14 @@ def test_group_norm_grad_pitches_and_alignment(pad_p, pad_s, offset, bf16):
         norm_grad_case(3, 120, C, G, bf16, gpu.ACT_RELU, pad_p=pad_p, pad_s=pad_s, offset=offset, seed=offset)
 
 
+@pytest.mark.parametrize("bf16,N,P,C,G", [(True, 1300, 784, 6, 3), (True, 1, 1000000, 3, 1), (True, 1100, 1024, 7, 7), (True, 3, 2500001, 1, 1),
+                                          (False, 1, 262144, 3, 3), (False, 700, 784, 6, 3), (False, 1300, 784, 3, 1), (False, 3, 600001, 2, 2)])
+def test_group_norm_of_few_channels_in_large_calls(bf16, N, P, C, G):
+    """Datasets of 28 x 28 x 6 maps, single RGB images: a position has fewer channels than a 16-byte vector, and the call more than 12 MB."""
+    norm_case(N, P, C, G, bf16, gpu.ACT_SILU, seed=C)
+    norm_grad_case(N, P, C, G, bf16, gpu.ACT_SILU, seed=C)
+
+
 @pytest.mark.parametrize("act", [gpu.ACT_NONE, gpu.ACT_GELU, gpu.ACT_SILU])
 def test_group_norm_grad_against_differences(act):
     norm_grad_case(3, 40, 24, 4, False, act, seed=9, differences=True)

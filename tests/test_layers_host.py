@@ -1,5 +1,8 @@
 """Argument checks of the layer operations' C entry points, and their scratch sizes; none of it reaches a device."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -163,3 +166,30 @@ def test_tensors_that_are_not_on_a_gpu_are_refused():
                  lambda: gpu.linear(x.int(), w, None, None, y)):
         with pytest.raises(ValueError):
             call()
+
+
+# Calls of abs_group_norm_scratch_bytes over every number of channels below and at a whole 16-byte vector, maps of a dataset, of single images
+# and of more than 12 MB, in a process of their own: a fault of the host code ends that one only.
+NORM_SCRATCH_SWEEP = """
+from paper_2301_08895_b200 import abs as gpu
+for channels in list(range(1, 10)) + [12, 13, 84, 255, 257, 4099]:
+    for groups in {1, channels, *(d for d in (2, 3, 4, 7) if channels % d == 0)}:
+        for samples, positions in ((1, 1), (20, 784), (700, 784), (1300, 784), (60000, 784), (1, 65536), (1, 262144), (1, 1000000), (1, 2 ** 31 - 1),
+                                   (2 ** 31 // groups - 1, 1), (3, 5)):
+            for dtype, size in ((gpu.FP32, 4), (gpu.BF16_FP32MASTER, 2)):
+                for grad in (False, True):
+                    n = gpu.group_norm_scratch_bytes(samples, positions, channels, groups, dtype, grad)
+                    if samples * positions * channels * size > 24e6:      # read twice: statistics of every group in between
+                        assert n >= samples * groups * 4 * (2 if grad else 3), (samples, positions, channels, groups, dtype, grad, n)
+for case in ((1300, 784, 6, 3, gpu.BF16_FP32MASTER, False), (700, 784, 6, 3, gpu.BF16_FP32MASTER, True), (1, 262144, 3, 3, gpu.FP32, False),
+             (1, 65536, 3, 3, gpu.FP32, True), (1, 1000000, 3, 1, gpu.BF16_FP32MASTER, False)):
+    gpu.group_norm_scratch_bytes(*case)
+print("swept")
+"""
+
+
+def test_group_norm_scratch_of_fewer_channels_than_a_vector():
+    out = subprocess.run([sys.executable, "-c", NORM_SCRATCH_SWEEP], capture_output=True, text=True, timeout=600,
+                         cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert out.returncode == 0, (out.returncode, out.stderr[-500:])
+    assert out.stdout.strip() == "swept"
