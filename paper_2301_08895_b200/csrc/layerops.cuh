@@ -185,8 +185,9 @@ template <int N> __device__ __forceinline__ Lanes<N> fma(const Lanes<N>& a, cons
 }
 // 1 / (1 + exp(-z)) of N values.  Two values share a reciprocal, 1 / a = b / (a b): a value then costs the special-function unit one
 // and a half instructions instead of two, which bounds a pass of SiLU over bf16 (64 x 64 x 64 x 320: 63.6 -> 55.6 us).
-// z is held at -41.5 from below (a NaN stays one), so that the product of two values of 1 + exp(-z) <= 2^60 stays finite: where it is held,
-// SiLU and its slope, both below 4e-17, are those of -41.5.
+// z is held at -41.5 from below, so that the product of two values of 1 + exp(-z) <= 2^60 stays finite.  held: z so held, a NaN kept; the
+// reciprocals take a NaN's exponential for 2^60 instead, since it would reach its partner through them, and the NaN comes back by the caller's
+// product with held.  SiLU and its slope, both below 4e-17 where z is held, are those of -41.5.
 template <int N> __device__ __forceinline__ Lanes<N> sigmoids(const Lanes<N>& z, Lanes<N>& held) {
   static_assert(N % 4 == 0, "pairs of pairs");
   float v[N];
@@ -199,7 +200,7 @@ template <int N> __device__ __forceinline__ Lanes<N> sigmoids(const Lanes<N>& z,
   held.set(v);
   mul(held, k).get(v);
 #pragma unroll
-  for (int j = 0; j < N; ++j) v[j] = ex2_approx(v[j]);
+  for (int j = 0; j < N; ++j) v[j] = fminf(ex2_approx(v[j]), 0x1p60f);
   a.set(v);
   a = add(a, one);
   Lanes<N> r;

@@ -739,6 +739,57 @@ def test_group_norm_keeps_nan_in_its_group(bf16):
         assert bool(bad[1, :, 8:16].all()) and int(bad.sum()) == P * 8
 
 
+def nan_at(t, *where):
+    """t is NaN at `where`, an index or mask, and finite elsewhere."""
+    torch = _torch()
+    mask = torch.zeros_like(t, dtype=torch.bool)
+    mask[where] = True
+    return bool(torch.isnan(t[mask]).all()) and bool(torch.isfinite(t[~mask]).all())
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("act", [gpu.ACT_GELU, gpu.ACT_SILU])
+@pytest.mark.parametrize("D", [1, 2, 3, 8])
+@pytest.mark.parametrize("P", [10, 200000])
+def test_group_norm_with_an_activation_keeps_nan_in_its_group(P, D, act, bf16):
+    """A NaN in x stays in its group, one in w or b in its channel; backward, one in x or w or b in its group's dx and its channel's dw and db
+    (in x also those of the group's other channels, through their xh)."""
+    torch = _torch()
+    d, C = dt(bf16), 48
+    G, c = C // D, 25
+    lo = c // D * D
+    group = slice(lo, lo + D)
+    for what in ("x", "w", "b"):
+        g = gen(D)
+        x, dy = randn(g, 2, P, C, dtype=d), randn(g, 2, P, C, dtype=d)
+        w, b = torch.ones(C, device="cuda", dtype=d), torch.zeros(C, device="cuda", dtype=d)
+        mean, rstd = torch.empty(2, G, device="cuda"), torch.empty(2, G, device="cuda")
+        y = torch.empty_like(x)
+        {"x": x[1, P // 2], "w": w, "b": b}[what][c] = float("nan")
+        gpu.group_norm(x, G, w, b, y, mean, rstd, 1e-5, act)
+        assert nan_at(y, 1, slice(None), group) if what == "x" else nan_at(y, slice(None), slice(None), c)
+        dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+        gpu.group_norm_grad(dy, x, G, w, b, mean, rstd, dx, dw, db, act)
+        assert nan_at(dx, 1, slice(None), group) if what == "x" else nan_at(dx, slice(None), slice(None), group)
+        channels = group if what == "x" else c
+        assert nan_at(dw, channels) and nan_at(db, channels)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("act", [gpu.ACT_GELU, gpu.ACT_SILU])
+def test_linear_grad_keeps_nan_in_its_column(act, bf16):
+    """A NaN in the saved pre-activation reaches its column of dw and db and its row of dx."""
+    torch = _torch()
+    d = dt(bf16)
+    for M, K, N in ((300, 40, 64), (300, 40, 63), (5, 24, 32), (1500, 1024, 1024)):
+        g = gen(M)
+        dy, x, w, z = randn(g, M, N, dtype=d), randn(g, M, K, dtype=d), randn(g, K, N, dtype=d), randn(g, M, N, dtype=d)
+        z[M // 2, N // 2 + 1] = float("nan")
+        dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(N, device="cuda", dtype=d)
+        gpu.linear_grad(dy, x, w, z, dx, dw, db, act)
+        assert nan_at(dx, M // 2) and nan_at(dw, slice(None), N // 2 + 1) and nan_at(db, N // 2 + 1)
+
+
 def norm_grad_case(N, P, C, G, bf16, act, affine=True, pad_p=0, pad_s=0, offset=0, seed=0, want=(True, True, True), in_place=False, differences=False):
     torch = _torch()
     g = gen(seed)
