@@ -790,6 +790,32 @@ def test_linear_grad_keeps_nan_in_its_column(act, bf16):
         assert nan_at(dx, M // 2) and nan_at(dw, slice(None), N // 2 + 1) and nan_at(db, N // 2 + 1)
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("n", [96, 95])
+def test_silu_slopes_far_above_zero_beside_smaller_ones(n, bf16):
+    """s (1 + z (1 - s)) for z of every size next to z of every other: 1 - s is exp(-z) s, not the rounding of s.  A slope of 1.1 at most, its
+    factors good to 2^-20."""
+    torch = _torch()
+    d, u = dt(bf16), half_step(bf16)
+    large = [12.0, 20.0, 30.0, 80.0, 1e3, 1e5, 1e8, 1e15, 1e30]
+    small = [-40.0, -3.0, 0.0, 0.3, 0.7, 1.5, 2.5, 5.0]
+    for shift in range(4):                                               # (which of its neighbours shares something with an element is the kernel's choice)
+        for big in large:
+            z = torch.tensor([big if (j >> 1) % 2 == shift % 2 and (j % 2 == 0 or shift > 1) else small[(j * 5 + shift) % 8] for j in range(n)], device="cuda").to(d)
+            slope = slope64(z.double(), gpu.ACT_SILU)
+            db, dw = torch.empty(n, device="cuda", dtype=d), torch.empty(16, n, device="cuda", dtype=d)
+            x = torch.zeros(4, 16, device="cuda", dtype=d)
+            x[0, 0] = 1.0
+            gpu.linear_grad(torch.ones(4, n, device="cuda", dtype=d), x, torch.zeros(16, n, device="cuda", dtype=d), z.expand(4, n).contiguous(), None, dw, db,
+                            gpu.ACT_SILU)
+            within(dw[0], slope, u * slope.abs() + 2 * E20)
+            within(db, 4 * slope, 4 * u * slope.abs() + 8 * E20)
+            x = torch.full((1, 64, n), 2.0, device="cuda", dtype=d)      # constant maps: u = b
+            mean, rstd = torch.full((1, 1), 2.0, device="cuda"), torch.ones(1, 1, device="cuda")
+            gpu.group_norm_grad(torch.ones_like(x), x, 1, None, z, mean, rstd, None, None, db, gpu.ACT_SILU)
+            within(db, 64 * slope, 64 * (u * slope.abs() + 2 * E20))
+
+
 def norm_grad_case(N, P, C, G, bf16, act, affine=True, pad_p=0, pad_s=0, offset=0, seed=0, want=(True, True, True), in_place=False, differences=False):
     torch = _torch()
     g = gen(seed)
