@@ -83,7 +83,13 @@ __device__ __forceinline__ float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float sigmoid(float z) { return rcp_approx(1.f + ex2_approx(-1.4426950408889634f * z)); }
+// z held at -41.5 from below, a NaN kept: SiLU and its slope are evaluated there, and below it they are those of -41.5, which are smaller than
+// 4e-17.  (Its exponential stays below 2^60, which the vectors' shared reciprocals need; -infinity gets a finite value.)
+__device__ __forceinline__ float silu_held(float z) {
+  float h;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(h) : "f"(z), "f"(-41.5f));
+  return h;
+}
 // Phi(z) and exp(-z^2 / 2): with x = |z| / sqrt(2), t = 1 / (1 + 0.3275911 x), erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2) + e,
 // |e| <= 1.5e-7 (Abramowitz and Stegun, 7.1.26); so Phi is good to 2^-23.
 __device__ __forceinline__ float normal_cdf(float z, float& bell) {
@@ -103,7 +109,10 @@ template <int ACT> __device__ __forceinline__ float act_value(float z) {
     float bell;
     return z * normal_cdf(z, bell);
   }
-  if (ACT == ABS_ACT_SILU) return z * sigmoid(z);
+  if (ACT == ABS_ACT_SILU) {
+    const float h = silu_held(z);
+    return h * rcp_approx(1.f + ex2_approx(-1.4426950408889634f * h));
+  }
   return z;
 }
 template <int ACT> __device__ __forceinline__ float act_slope(float z) {
@@ -113,9 +122,9 @@ template <int ACT> __device__ __forceinline__ float act_slope(float z) {
     const float c = normal_cdf(z, bell);
     return fmaf(0.39894228040143268f * z, bell, c);
   }
-  if (ACT == ABS_ACT_SILU) {
-    const float s = sigmoid(z);
-    return s * fmaf(z, 1.f - s, 1.f);
+  if (ACT == ABS_ACT_SILU) {                           // s (1 + z (1 - s)) with 1 - s = exp(-z) s: far above zero 1 - s would be s's rounding
+    const float h = silu_held(z), e = ex2_approx(-1.4426950408889634f * h), s = rcp_approx(1.f + e);
+    return s * fmaf(h * e, s, 1.f);
   }
   return 1.f;
 }
@@ -185,9 +194,8 @@ template <int N> __device__ __forceinline__ Lanes<N> fma(const Lanes<N>& a, cons
 }
 // 1 / (1 + exp(-z)) of N values, and e = exp(-z).  Two values share a reciprocal, 1 / a = b / (a b): a value then costs the special-function unit one
 // and a half instructions instead of two, which bounds a pass of SiLU over bf16 (64 x 64 x 64 x 320: 63.6 -> 55.6 us).
-// z is held at -41.5 from below, so that the product of two values of 1 + exp(-z) <= 2^60 stays finite.  held: z so held, a NaN kept; the
-// reciprocals take a NaN's exponential for 2^60 instead, since it would reach its partner through them, and the NaN comes back by the caller's
-// product with held.  SiLU and its slope, both below 4e-17 where z is held, are those of -41.5.
+// held: z as silu_held gives it, so that the product of two values of 1 + exp(-z) <= 2^60 stays finite; the reciprocals take a NaN's exponential
+// for 2^60 instead, since it would reach its partner through them, and the NaN comes back by the caller's product with held.
 template <int N> __device__ __forceinline__ Lanes<N> sigmoids(const Lanes<N>& z, Lanes<N>& held, Lanes<N>& e) {
   static_assert(N % 4 == 0, "pairs of pairs");
   float v[N];
@@ -196,7 +204,7 @@ template <int N> __device__ __forceinline__ Lanes<N> sigmoids(const Lanes<N>& z,
   one.fill(1.f);
   z.get(v);
 #pragma unroll
-  for (int j = 0; j < N; ++j) asm("max.NaN.f32 %0, %1, %2;" : "=f"(v[j]) : "f"(v[j]), "f"(-41.5f));
+  for (int j = 0; j < N; ++j) v[j] = silu_held(v[j]);
   held.set(v);
   mul(held, k).get(v);
 #pragma unroll
@@ -239,7 +247,7 @@ template <int ACT, int N> __device__ __forceinline__ Lanes<N> act_slopes(const L
     Lanes<N> held, e, one;
     one.fill(1.f);
     const Lanes<N> s = sigmoids(z, held, e);
-    return mul(s, fma(mul(held, e), s, one));          // s (1 + z (1 - s)) with 1 - s = exp(-z) s: far above zero 1 - s would be s's rounding
+    return mul(s, fma(mul(held, e), s, one));          // (as act_slope)
   }
   float v[N];
   Lanes<N> r;

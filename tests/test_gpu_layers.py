@@ -1161,3 +1161,43 @@ def test_layer_operations_refuse_wrong_tensors():
     assert e.value.code == gpu.EINVAL
     with pytest.raises(ValueError):
         gpu.group_norm(m, 4, torch.ones(8, device="cuda"), None, m, None, None)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_silu_is_one_function(bf16):
+    """Values and slopes far below zero, at -infinity and at NaN are the same wherever they are formed: element by element or in vectors, in
+    the layer of a few or many rows, in its gradient and in group norm."""
+    torch = _torch()
+    d = dt(bf16)
+    z = [-30.0, -41.0, -42.0, -60.0, -88.0, -90.0, -200.0, -1e4, -1e30, -float("inf"), float("nan"), -41.4]
+    vals, slopes = [], []
+    for n in (96, 95):                                       # whole vectors, or not
+        zt = torch.tensor([z[j % len(z)] for j in range(n)], device="cuda").to(d)
+        for rows in (1, 5, 300):
+            y = torch.empty(rows, n, device="cuda", dtype=d)
+            gpu.linear(torch.zeros(rows, 16, device="cuda", dtype=d), torch.zeros(16, n, device="cuda", dtype=d), zt, None, y, gpu.ACT_SILU)
+            vals.append(y[rows - 1, :len(z)])
+            db = torch.empty(n, device="cuda", dtype=d)
+            dy = torch.zeros(rows, n, device="cuda", dtype=d)
+            dy[rows - 1] = 1.0
+            gpu.linear_grad(dy, torch.zeros(rows, 16, device="cuda", dtype=d), torch.zeros(16, n, device="cuda", dtype=d), zt.expand(rows, n).contiguous(),
+                            None, None, db, gpu.ACT_SILU)
+            slopes.append(db[:len(z)])
+        for P in (1, 400000):
+            x = torch.full((1, P, n), 2.0, device="cuda", dtype=d)        # constant maps: u = b
+            y, st = torch.empty_like(x), [torch.empty(1, 1, device="cuda") for _ in range(2)]
+            gpu.group_norm(x, 1, None, zt, y, *st, 1.0, gpu.ACT_SILU)
+            vals.append(y[0, P - 1, :len(z)])
+            dy = torch.zeros_like(x)
+            dy[0, P // 2] = 1.0
+            gpu.group_norm_grad(dy, x, 1, None, zt, *st, None, None, db, gpu.ACT_SILU)
+            slopes.append(db[:len(z)])
+    for got in (vals, slopes):
+        first = got[0].double()
+        assert bool(torch.isnan(first[10])) and bool(torch.isfinite(torch.cat([first[:10], first[11:]])).all())
+        # (the reciprocal shared with another partner is another rounding: rcp 2^-22, two products 2^-24 each)
+        assert 0 < -float(first[2]) < 4e-17 and bool(((first[2:10] / first[2] - 1).abs() <= 2.0 ** -19).all())
+        for other in got[1:]:                                # (the two forms of the reciprocal differ by roundings; u for a step of bf16)
+            assert bool(torch.isnan(other[10]))
+            keep = [i for i in range(len(z)) if i != 10]
+            within(other[keep], first[keep], (2.0 ** -19 + (2 * half_step(bf16) if bf16 else 0.0)) * first[keep].abs())
