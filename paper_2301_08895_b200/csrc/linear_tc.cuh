@@ -14,7 +14,8 @@
 // Persistent and warp-specialised: warp 0 issues the copies of a ring of stages, warp 1 the products into two alternating
 // accumulators in tensor memory, warps 2..9 take the other accumulator through the epilogue meanwhile: registers, a box of 32
 // rows x 128 bytes per warp in shared memory, one bulk store per box.  CG = 2: a cluster of two CTAs shares a tile of 256 x BN,
-// each loads its own rows of A and half of B.  A sum can be split over `splits` tiles that leave fp32 partial results.
+// each loads its own rows of A and half of B.  A sum can be split over `splits` tiles that leave fp32 partial results, and products of pieces leave
+// tensor memory in stretches (below).
 // Every wait is bounded: on expiry the CTA raises the operations' status word, drains its copies, frees tensor memory and returns.
 #pragma once
 #include "layerops.cuh"
@@ -28,6 +29,13 @@ using namespace tc;
 
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
+
+// An addition in tensor memory truncates, a step of 2^-23 of the sum towards zero, and in a long sum the steps add up: a product of pieces over 20000
+// terms of one sign was off by 9.7e-5.  So products of pieces add up there over a stretch of blocks only; the epilogue's warps take each stretch out
+// and add it in registers, rounding to nearest, while the next one runs.  SMALL_STRETCH in the passes of the smaller pairs, whose steps count 2^-7 and
+// less, STRETCH in the last pass: with 8, 4 or 2 blocks that product is off by 2.6e-7, 1.4e-7 or 2.0e-7 (one of both signs by 4.9e-7, 2.8e-7 or 2.6e-7
+// of its size; on FP32 FMAs 1.1e-6 and 1.8e-6) and takes (2048 x 20000 x 1024) 470, 490 or 515 us, 476 in one stretch.
+constexpr int SMALL_STRETCH = 64, STRETCH = 4;
 
 struct Args {
   int a_mn, b_mn;                        // operand layouts: 0 K-major, 1 MN-major
@@ -103,6 +111,13 @@ __device__ __forceinline__ void box_rows_out(const uint8_t* box, int lane, __nv_
     if (j < J) d[0] = b.x;
     if (j + 1 < J) d[1] = b.y;
   }
+}
+
+// First block behind the stretch that starts with block kb, of a tile's blocks in front of `end`.
+__device__ __forceinline__ int stretch_end(const Args& p, int kb, int end) {
+  const int small = p.n_kb - p.kb_pass;
+  if (kb < small) return min(min((kb / SMALL_STRETCH + 1) * SMALL_STRETCH, small), end);
+  return min(small + ((kb - small) / STRETCH + 1) * STRETCH, end);
 }
 
 // PIECES: fp32 operands in pieces, partial results; an own instance, since the passes' bookkeeping costs the bf16 products 3 % (205 us for 199).
@@ -244,29 +259,32 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
       const uint32_t a_kstep = p.a_mn ? 2048u : 32u, b_kstep = p.b_mn ? 2048u : 32u;
       for (int t = unit; t < p.n_tiles && ok; t += n_units) {
         const Tile c = tile_of(t);
-        if (!mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort)) break;
-        tc_fence_after();
-        const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
-        for (int kb = 0; kb < c.n_kb; ++kb) {
-          if (!mbar_wait(&full[stage], phase, abort)) { ok = false; break; }
+        for (int kb = 0; kb < c.n_kb && ok;) {
+          const int first = kb, stop = PIECES ? stretch_end(p, c.kb0 + kb, c.kb0 + c.n_kb) - c.kb0 : c.n_kb;
+          if (!mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t sa = base + (uint32_t)stage * C::STAGE_BYTES, sb = sa + C::A_BYTES;
+          const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
+          for (; kb < stop; ++kb) {
+            if (!mbar_wait(&full[stage], phase, abort)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t sa = base + (uint32_t)stage * C::STAGE_BYTES, sb = sa + C::A_BYTES;
 #pragma unroll
-          for (int kk = 0; kk < BK / UK; ++kk) {
-            const uint64_t da = smem_desc(sa + kk * a_kstep, a_lbo, 1024u);
-            const uint64_t db = smem_desc(sb + kk * b_kstep, b_lbo, 1024u);
-            if (CG == 2) umma2(d_tmem, da, db, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
-            else umma(d_tmem, da, db, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+            for (int kk = 0; kk < BK / UK; ++kk) {
+              const uint64_t da = smem_desc(sa + kk * a_kstep, a_lbo, 1024u);
+              const uint64_t db = smem_desc(sb + kk * b_kstep, b_lbo, 1024u);
+              if (CG == 2) umma2(d_tmem, da, db, idesc, (kb > first || kk > 0) ? 1u : 0u);
+              else umma(d_tmem, da, db, idesc, (kb > first || kk > 0) ? 1u : 0u);
+            }
+            if (CG == 2) umma2_commit_both(&empty[stage]);
+            else umma_commit(&empty[stage]);
+            if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
           }
-          if (CG == 2) umma2_commit_both(&empty[stage]);
-          else umma_commit(&empty[stage]);
-          if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+          if (!ok) break;
+          if (CG == 2) umma2_commit_both(&acc_full[acc]);
+          else umma_commit(&acc_full[acc]);
+          acc ^= 1;
+          if (acc == 0) acc_phase ^= 1u;
         }
-        if (!ok) break;
-        if (CG == 2) umma2_commit_both(&acc_full[acc]);
-        else umma_commit(&acc_full[acc]);
-        acc ^= 1;
-        if (acc == 0) acc_phase ^= 1u;
       }
     }
   } else {
@@ -281,30 +299,75 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     uint8_t* my_row = my_box + lane * 128;
     int acc = 0;
     uint32_t acc_phase = 0;
+    auto release = [&] {                       // the accumulator is drained; its barrier lives in the leader CTA
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (CG == 2) mbar_arrive_cluster(acc_empty0_addr + 8u * (uint32_t)acc);
+        else mbar_arrive(&acc_empty[acc]);
+      }
+      acc ^= 1;
+      if (acc == 0) acc_phase ^= 1u;
+    };
+    auto partial_box = [&](const uint32_t* v, int col, int row0, int split) {      // 32 columns of a partial result
+      if (lane == 0) bulk_wait_read();         // the box is free once the store issued from it has read it
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        *reinterpret_cast<uint4*>(my_row + ((j ^ sw) << 4)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+      fence_async();
+      __syncwarp();
+      if (lane == 0) {
+        asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                     ::"l"(reinterpret_cast<uint64_t>(&map_out)), "r"(smem_u32(my_box)), "r"(col), "r"(row0), "r"(split) : "memory");
+        bulk_commit();
+      }
+    };
     for (int t = unit; t < p.n_tiles; t += n_units) {
       const Tile c = tile_of(t);
       const int row0 = c.i0 + q * 32, row = row0 + lane;
+      if constexpr (PIECES) {
+        const int j0 = c.j0 + half * HALF_COLS;
+        uint32_t sum[HALF_COLS];               // (binary32)
+#pragma unroll
+        for (int i = 0; i < HALF_COLS; ++i) sum[i] = 0u;
+        bool ok = true;
+        for (int kb = 0; kb < c.n_kb;) {
+          kb = stretch_end(p, c.kb0 + kb, c.kb0 + c.n_kb) - c.kb0;
+          ok = mbar_wait(&acc_full[acc], acc_phase, abort);
+          if (!ok) break;
+          tc_fence_after();
+          if (works && row0 < p.I) {           // (uniform in the warp)
+            const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN + half * HALF_COLS);
+#pragma unroll
+            for (int c0 = 0; c0 < HALF_COLS; c0 += 32)
+              if (j0 + c0 < p.J) {
+                uint32_t v[32];
+                tmem_ld32(t_row + (uint32_t)c0, v);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) sum[c0 + i] = __float_as_uint(__uint_as_float(sum[c0 + i]) + __uint_as_float(v[i]));
+              }
+          }
+          release();
+        }
+        if (!ok) break;
+        if (works && row0 < p.I) {
+#pragma unroll
+          for (int c0 = 0; c0 < HALF_COLS; c0 += 32)
+            if (j0 + c0 < p.J) partial_box(&sum[c0], j0 + c0, row0, c.split);
+        }
+        continue;
+      }
       if (!mbar_wait(&acc_full[acc], acc_phase, abort)) break;
       tc_fence_after();
       const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN);
       if (works && row0 < p.I) {               // (uniform in the warp)
-        if (PIECES || p.partial) {
+        if (p.partial) {
 #pragma unroll 1
           for (int c0 = half * HALF_COLS; c0 < (half + 1) * HALF_COLS && c.j0 + c0 < p.J; c0 += 32) {
             uint32_t v[32];
             tmem_ld32(t_row + (uint32_t)c0, v);
-            if (lane == 0) bulk_wait_read();   // the box is free once the store issued from it has read it
-            __syncwarp();
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              *reinterpret_cast<uint4*>(my_row + ((j ^ sw) << 4)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-            fence_async();
-            __syncwarp();
-            if (lane == 0) {
-              asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
-                           ::"l"(reinterpret_cast<uint64_t>(&map_out)), "r"(smem_u32(my_box)), "r"(c.j0 + c0), "r"(row0), "r"(c.split) : "memory");
-              bulk_commit();
-            }
+            partial_box(v, c.j0 + c0, row0, c.split);
           }
         } else {
 #pragma unroll 1
@@ -392,14 +455,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
           }
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {                         // the accumulator barrier lives in the leader CTA
-        if (CG == 2) mbar_arrive_cluster(acc_empty0_addr + 8u * (uint32_t)acc);
-        else mbar_arrive(&acc_empty[acc]);
-      }
-      acc ^= 1;
-      if (acc == 0) acc_phase ^= 1u;
+      release();
     }
     if (lane == 0) bulk_wait_read();           // shared memory may go once the stores have read it
   }

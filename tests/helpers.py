@@ -156,3 +156,29 @@ def compare_with_oracle(cfg, X, y, w0, rounds, tol, forced=False, loss_tol=None,
         assert np.all(np.abs(la - lb) <= lt * np.maximum(1.0, np.abs(lb))), \
             "uploaded losses differ in round %d" % t
     return rows, orows, err, o
+
+
+def one_product_operands(M, K, N, seed):
+    """float32 (x [M, K], w [K, N]): a row of x has one element that is not zero, and every such element and every element of w uses all 24 bits of
+    its significand, over 2^40 of magnitudes: (x w)[i, j] is one product."""
+    g = np.random.default_rng(seed)
+
+    def full(*shape):
+        bits = g.integers(1 << 22, 1 << 23, shape) * 2 + 1              # odd, 24 bits
+        return (bits * np.exp2(g.integers(-44, -4, shape)) * g.choice([-1.0, 1.0], shape)).astype(np.float32)
+    x = np.zeros((M, K), np.float32)
+    x[np.arange(M), (np.arange(M) * 7 + 3) % K] = full(M)
+    return x, full(K, N)
+
+
+def bf16_pieces(v):
+    """A float32 array as three bf16 numbers per element (as float64) whose sum it is."""
+    def nearest(a):                                                     # float32 to bf16, ties to even
+        u = a.astype(np.float32).view(np.uint32)
+        return ((u + 0x7FFF + ((u >> 16) & 1)) & np.uint32(0xFFFF0000)).view(np.float32)
+    first = nearest(v)
+    rest = v - first
+    second = nearest(rest)
+    third = rest - second
+    assert np.array_equal(nearest(third), third)
+    return [p.astype(np.float64) for p in (first, second, third)]

@@ -10,6 +10,7 @@ import math
 import numpy as np
 import pytest
 
+import helpers
 from oracle import philox
 from paper_2301_08895_b200 import abs as gpu
 
@@ -338,6 +339,60 @@ def test_linear_grad_fp32_in_pieces(M, K, N, pad, offset):
     grad_case(M, K, N, False, gpu.ACT_GELU, pad=pad, offset=offset, seed=M)
     for want in ((True, False, False), (False, True, False), (False, False, True), (True, False, True), (False, True, True)):
         grad_case(M, K, N, False, gpu.ACT_NONE, pad=pad, offset=offset, seed=M, want=want)
+
+
+def test_linear_fp32_in_pieces_of_single_products():
+    """Sums of one product each, in the three layouts: what the three pairs left out make up (2^-23 of it) and a rounding."""
+    torch = _torch()
+    M, K, N = 520, 1024, 1030
+    assert takes_pieces(M, K, N) and takes_pieces(M, K, N, True)
+    dev = lambda a: torch.from_numpy(a).cuda()                          # noqa: E731
+    x, w = map(dev, helpers.one_product_operands(M, K, N, 1))
+    y = torch.empty(M, N, device="cuda")
+    gpu.linear(x, w, None, None, y)
+    want = x.double() @ w.double()
+    within(y, want, 2.0 ** -22 * want.abs())
+    dy, wt = map(dev, helpers.one_product_operands(M, N, K, 2))         # dx = dy w^T
+    dx = torch.empty(M, K, device="cuda")
+    gpu.linear_grad(dy, x, wt.t().contiguous(), None, dx, None, None)
+    want = dy.double() @ wt.double()
+    within(dx, want, 2.0 ** -22 * want.abs())
+    xt, dy = map(dev, helpers.one_product_operands(K, M, N, 3))         # dw = x^T dy
+    dw = torch.empty(K, N, device="cuda")
+    gpu.linear_grad(dy, xt.t().contiguous(), w, None, None, dw, None)
+    want = xt.double() @ dy.double()
+    within(dw, want, 2.0 ** -22 * want.abs())
+
+
+@pytest.mark.parametrize("one_sign", [False, True])
+@pytest.mark.parametrize("layout", ["y", "dx", "dw"])
+@pytest.mark.parametrize("K", [785, 4096, 20000])
+def test_linear_fp32_in_pieces_does_not_drift(K, layout, one_sign):
+    """The tensor cores' accumulator truncates: a sum of 16 products and itself loses up to 2^-23 of itself, half of it on average.  It takes 256
+    terms, 16 such additions, before the parts are added to nearest: of a part whose terms have one sign, that is at most 8 2^-23, on average half of it;
+    the K / 256 additions behind add at most K / 512 2^-24.  Terms of both signs: an addition loses up to 2^-23, on average half, of a partial sum of
+    up to 16 terms' size, two thirds of that on average: 16 * 10.7 * 2^-24 for each of K / 256 independent parts, 10.7 sqrt(K) 2^-24 of a term."""
+    torch = _torch()
+    M, N = 512, 640
+    g = gen(K)
+    draw = (lambda *s: torch.rand(*s, generator=g, device="cuda") + 0.5) if one_sign else (lambda *s: torch.randn(*s, generator=g, device="cuda"))
+    a, b = draw(M, K), draw(K, N)
+    got, want = torch.empty(M, N, device="cuda"), a.double() @ b.double()
+    if layout == "y":
+        assert takes_pieces(M, K, N)
+        gpu.linear(a, b, None, None, got)
+    elif layout == "dx":
+        assert takes_pieces(M, N, K, True)
+        gpu.linear_grad(a, torch.empty(M, N, device="cuda"), b.t().contiguous(), None, got, None, None)
+    else:
+        assert takes_pieces(K, M, N, True)
+        gpu.linear_grad(b, a.t().contiguous(), torch.empty(M, N, device="cuda"), None, None, got, None)
+    err = got.double() - want
+    if one_sign:
+        assert abs(float((err / want).mean())) <= 2.0 ** -21
+        within(got, want, (2.0 ** -20 + K / 512 * 2.0 ** -24 + 2.0 ** -22) * want)
+    else:
+        assert float(err.square().mean().sqrt()) <= 12 * math.sqrt(K) * 2.0 ** -24
 
 
 def test_linear_fp32_of_what_pieces_cannot_hold():

@@ -7,6 +7,7 @@ import sys
 import numpy as np
 import pytest
 
+import helpers
 from paper_2301_08895_b200 import abs as gpu
 from paper_2301_08895_b200 import build
 
@@ -193,3 +194,18 @@ def test_group_norm_scratch_of_fewer_channels_than_a_vector():
                          cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     assert out.returncode == 0, (out.returncode, out.stderr[-500:])
     assert out.stdout.strip() == "swept"
+
+
+PAIRS = ((0, 2), (2, 0), (1, 1), (0, 1), (1, 0), (0, 0))                # the pairs of pieces that a product is taken as
+
+
+def test_the_bound_of_products_in_pieces_sees_each_pair():
+    """On the operands of the exact test of fp32 products in pieces: six pairs stay within 2^-22 of the product, any five do not."""
+    x, w = helpers.one_product_operands(520, 64, 130, 5)
+    a, b = helpers.bf16_pieces(x), helpers.bf16_pieces(w)
+    want = x.astype(np.float64) @ w.astype(np.float64)
+    terms = {p: a[p[0]] @ b[p[1]] for p in PAIRS}
+    total = sum(terms.values())
+    assert np.all(np.abs(total - want) <= 2.0 ** -23 * np.abs(want))
+    for p in PAIRS:
+        assert np.mean(np.abs(total - terms[p] - want) > 2.0 ** -22 * np.abs(want)) > 0.8
