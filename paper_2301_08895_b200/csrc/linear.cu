@@ -231,7 +231,7 @@ template <typename T> cudaError_t finish(const float* part, int splits, int I, i
   f.bias = r.bias; f.res = r.res; f.out = r.out; f.pre = r.pre;
   f.ldr = r.ldr; f.ldo = r.ldo; f.ldp = r.ldp;
   f.quads = Divisor((uint32_t)(f.Jp / 4));
-  f.n = (uint32_t)((size_t)I * (f.Jp / 4));              // (partial results hold at most 2^28 floats)
+  f.n = (uint32_t)((size_t)I * (f.Jp / 4));              // (at most 2^31: plan_product)
   const unsigned blocks = (f.n + 255) / 256;
   return launch(ACT_FN(FinishFn, finish_kernel, r.act, T), dim3(blocks < 8u * sms ? blocks : 8u * sms), 256, 0, 1, s, f);
 }
@@ -239,7 +239,7 @@ template <typename T> cudaError_t finish(const float* part, int splits, int I, i
 // ------------------------------------------------------------------ tensor-core products (bf16)
 
 // How a product C[I][J] = sum over K terms is cut up.
-struct Plan { int bn, cg, splits, kb_per; size_t part_bytes; double t; };
+struct Plan { int bn, cg, splits, kb_per; size_t part_bytes; double t; bool stretches; };     // stretches: of sums too long for tensor memory in one
 
 // The cheapest of the five tiles and of the ways to split the sum, by a model in microseconds: a block of 64 terms of a tile (measured
 // at 8192 x 4096 x 4096: 178 us with 256 x 256 tiles of CTA pairs; the narrow tiles wait for operands, not for the tensor cores), the
@@ -263,10 +263,15 @@ Plan plan_product(long long I, int J, long long K, bool partial = false) {
       if (s > 1 || partial) t += 2.5 + (double)s * I * Jp * 8.0 / 6e6;
       if (t < best_t) {
         best_t = t;
-        best = Plan{o.bn, o.cg, s, (int)per, s > 1 || partial ? round256((size_t)s * I * Jp * 4) : 0, t};
+        best = Plan{o.bn, o.cg, s, (int)per, s > 1 || partial ? round256((size_t)s * I * Jp * 4) : 0, t, partial};
       }
       if (tiles * s >= 2 * units) break;
     }
+  }
+  // (so that finish_kernel's numbers stay below 2^32; with larger results, a device of 180 GB holds operands of fewer than 7000 blocks)
+  if (best.kb_per > dense::LONG_SUM && I * Jp <= 1ll << 33) {
+    best.stretches = true;
+    best.part_bytes = round256((size_t)best.splits * I * Jp * 4);
   }
   return best;
 }
@@ -314,11 +319,11 @@ bool tma_able(const void* p, long long rows, long long ld) { return (uintptr_t)p
 long long tma_pitch(long long rows, long long cols, long long ld) { return rows == 1 ? (cols + 7) / 8 * 8 : ld; }
 size_t pack_bytes(long long rows, long long cols) { return round256((size_t)rows * ((cols + 7) / 8 * 8) * 2); }
 
-template <int BN, int CG, bool PIECES>
+template <int BN, int CG, bool STRETCHES>
 cudaError_t launch_dense(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const CUtensorMap& z, const dense::Args& p, int sms, int device,
                          cudaStream_t s) {
   static std::atomic<uint64_t> ready;
-  auto* kernel = dense::dense_kernel<BN, CG, PIECES>;
+  auto* kernel = dense::dense_kernel<BN, CG, STRETCHES>;
   if (!(ready.load(std::memory_order_acquire) >> device & 1)) {
     const cudaError_t e = allow_smem(kernel, dense::Cfg<BN, CG>::SMEM_BYTES);
     if (e != cudaSuccess) return e;
@@ -328,12 +333,12 @@ cudaError_t launch_dense(const CUtensorMap& a, const CUtensorMap& b, const CUten
   return launch(kernel, dim3((unsigned)(units * CG)), dense::THREADS, dense::Cfg<BN, CG>::SMEM_BYTES, CG, s, a, b, o, z, p);
 }
 
-template <bool PIECES>
+template <bool STRETCHES>
 cudaError_t launch_tile(const Plan& pl, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const CUtensorMap& z, const dense::Args& p, int sms,
                         int device, cudaStream_t s) {
-  if (pl.cg == 2) return pl.bn == 256 ? launch_dense<256, 2, PIECES>(a, b, o, z, p, sms, device, s) : launch_dense<128, 2, PIECES>(a, b, o, z, p, sms, device, s);
-  return pl.bn == 256 ? launch_dense<256, 1, PIECES>(a, b, o, z, p, sms, device, s)
-         : pl.bn == 128 ? launch_dense<128, 1, PIECES>(a, b, o, z, p, sms, device, s) : launch_dense<64, 1, PIECES>(a, b, o, z, p, sms, device, s);
+  if (pl.cg == 2) return pl.bn == 256 ? launch_dense<256, 2, STRETCHES>(a, b, o, z, p, sms, device, s) : launch_dense<128, 2, STRETCHES>(a, b, o, z, p, sms, device, s);
+  return pl.bn == 256 ? launch_dense<256, 1, STRETCHES>(a, b, o, z, p, sms, device, s)
+         : pl.bn == 128 ? launch_dense<128, 1, STRETCHES>(a, b, o, z, p, sms, device, s) : launch_dense<64, 1, STRETCHES>(a, b, o, z, p, sms, device, s);
 }
 
 __device__ int g_status;                 // set by a kernel whose bounded wait ran out; read and cleared by abs_op_status
@@ -359,6 +364,7 @@ int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, in
     p.a_step = (int)(a.rows / 3); p.b_step = (int)(b.rows / 3);
   }
   p.splits = pl.splits; p.kb_per = pl.kb_per;
+  p.stretch = pieces ? dense::STRETCH : dense::LONG_STRETCH;
   p.n_it = (I + 128 * pl.cg - 1) / (128 * pl.cg);
   p.n_jt = (J + pl.bn - 1) / pl.bn;
   const long long n_tiles = (long long)p.n_it * p.n_jt * pl.splits;
@@ -368,7 +374,8 @@ int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, in
   if (!p.status) return fail(ABS_ECUDA, "cudaGetSymbolAddress(status) failed");
   CUtensorMap ma, mb, mo, mz;
   bool ok = matrix_map(&ma, a.p, a.rows, a.cols, a.ld, a_mn ? 64 : 128) && matrix_map(&mb, b.p, b.rows, b.cols, b.ld, b_mn ? 64 : pl.bn / pl.cg);
-  if (pl.splits > 1 || pieces) {
+  const bool partial = pl.splits > 1 || pl.stretches;
+  if (partial) {
     p.partial = 1;
     ok = ok && partial_map(&mo, part, I, J, Jp, pl.splits);
   } else {
@@ -385,9 +392,9 @@ int tc_product(const Operand& a, int a_mn, const Operand& b, int b_mn, int I, in
   mz = mo;
   if (p.pre_tma) ok = ok && matrix_map(&mz, r.pre, I, J, tma_pitch(I, J, r.ldp), 32);
   if (!ok) return fail(ABS_ECUDA, "cuTensorMapEncodeTiled failed");
-  auto* go = pieces ? &launch_tile<true> : &launch_tile<false>;
+  auto* go = pl.stretches ? &launch_tile<true> : &launch_tile<false>;
   cudaError_t e = go(pl, ma, mb, mo, mz, p, sms, device, s);
-  if (e == cudaSuccess && pl.splits > 1 && !pieces) e = finish<__nv_bfloat16>(part, pl.splits, I, J, r, sms, s);
+  if (e == cudaSuccess && partial && !pieces) e = finish<__nv_bfloat16>(part, pl.splits, I, J, r, sms, s);
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }
 

@@ -35,13 +35,16 @@ constexpr int THREADS = 64 + 32 * EPI_WARPS;
 // and add it in registers, rounding to nearest, while the next one runs.  SMALL_STRETCH in the passes of the smaller pairs, whose steps count 2^-7 and
 // less, STRETCH in the last pass: with 8, 4 or 2 blocks that product is off by 2.6e-7, 1.4e-7 or 2.0e-7 (one of both signs by 4.9e-7, 2.8e-7 or 2.6e-7
 // of its size; on FP32 FMAs 1.1e-6 and 1.8e-6) and takes (2048 x 20000 x 1024) 470, 490 or 515 us, 476 in one stretch.
-constexpr int SMALL_STRETCH = 64, STRETCH = 4;
+// A sum in bf16 is rounded by up to 2^-8 and left in one stretch up to LONG_SUM blocks (65536 terms of one sign: off by 4e-4); longer ones go in
+// stretches of LONG_STRETCH (off by 8e-6; 134 million terms 1.4e-2 before), which also keeps the epilogue's wait for a stretch below half a millisecond.
+constexpr int SMALL_STRETCH = 64, STRETCH = 4, LONG_SUM = 1024, LONG_STRETCH = 64;
 
 struct Args {
   int a_mn, b_mn;                        // operand layouts: 0 K-major, 1 MN-major
   int I, J, n_kb;                        // rows and columns of C; blocks of 64 terms of the sum
   int splits, kb_per;                    // tiles that share a sum, blocks of each
   int kb_pass, a_step, b_step;           // blocks of one pair of pieces; rows from a piece to the next (0: bf16, one pass)
+  int stretch;                           // STRETCHES: blocks of a stretch of the last pass
   int n_it, n_jt, n_tiles;
   // final results (splits = 1)
   const __nv_bfloat16* bias; const __nv_bfloat16* res; __nv_bfloat16* out; __nv_bfloat16* pre;
@@ -117,11 +120,12 @@ __device__ __forceinline__ void box_rows_out(const uint8_t* box, int lane, __nv_
 __device__ __forceinline__ int stretch_end(const Args& p, int kb, int end) {
   const int small = p.n_kb - p.kb_pass;
   if (kb < small) return min(min((kb / SMALL_STRETCH + 1) * SMALL_STRETCH, small), end);
-  return min(small + ((kb - small) / STRETCH + 1) * STRETCH, end);
+  return min(small + ((kb - small) / p.stretch + 1) * p.stretch, end);
 }
 
-// PIECES: fp32 operands in pieces, partial results; an own instance, since the passes' bookkeeping costs the bf16 products 3 % (205 us for 199).
-template <int BN, int CG, bool PIECES>
+// STRETCHES: sums that leave tensor memory in stretches, partial results: fp32 operands in pieces, long sums in bf16; an own instance, since the
+// bookkeeping costs the other bf16 products 3 % (205 us for 199).
+template <int BN, int CG, bool STRETCHES>
 __global__ void __launch_bounds__(THREADS, 1)
 dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
              const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_pre, const __grid_constant__ Args p) {
@@ -203,7 +207,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
           ra = p.a_step * (int)(split3::A_PIECE >> 4 * pass & 15u);
           rb = p.b_step * (int)(split3::B_PIECE >> 4 * pass & 15u);
         };
-        if (PIECES) {
+        if (STRETCHES) {
           pass = at / p.kb_pass;
           at -= pass * p.kb_pass;
           pieces();
@@ -216,7 +220,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             mbar_expect_tx(&full[stage], CG * C::STAGE_BYTES);
             armed[stage] = (int)phase;
           }
-          const int k0 = PIECES ? at * BK : (c.kb0 + kb) * BK;
+          const int k0 = STRETCHES ? at * BK : (c.kb0 + kb) * BK;
           if (p.a_mn) {
             for (int j = 0; j < BM / 64; ++j) load(sa + j * 8192, &map_a, stage, c.i0 + 64 * j, k0 + ra);
           } else {
@@ -227,7 +231,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
           } else {
             load(sb, &map_b, stage, k0, j0 + rb);
           }
-          if (PIECES && ++at == p.kb_pass) {
+          if (STRETCHES && ++at == p.kb_pass) {
             at = 0;
             ++pass;
             pieces();
@@ -260,7 +264,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
       for (int t = unit; t < p.n_tiles && ok; t += n_units) {
         const Tile c = tile_of(t);
         for (int kb = 0; kb < c.n_kb && ok;) {
-          const int first = kb, stop = PIECES ? stretch_end(p, c.kb0 + kb, c.kb0 + c.n_kb) - c.kb0 : c.n_kb;
+          const int first = kb, stop = STRETCHES ? stretch_end(p, c.kb0 + kb, c.kb0 + c.n_kb) - c.kb0 : c.n_kb;
           if (!mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort)) { ok = false; break; }
           tc_fence_after();
           const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
@@ -326,7 +330,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     for (int t = unit; t < p.n_tiles; t += n_units) {
       const Tile c = tile_of(t);
       const int row0 = c.i0 + q * 32, row = row0 + lane;
-      if constexpr (PIECES) {
+      if constexpr (STRETCHES) {
         const int j0 = c.j0 + half * HALF_COLS;
         uint32_t sum[HALF_COLS];               // (binary32)
 #pragma unroll

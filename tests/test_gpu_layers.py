@@ -395,6 +395,45 @@ def test_linear_fp32_in_pieces_does_not_drift(K, layout, one_sign):
         assert float(err.square().mean().sqrt()) <= 12 * math.sqrt(K) * 2.0 ** -24
 
 
+def test_linear_grad_bf16_over_many_rows():
+    """134 million rows of one sign: the sum in bf16 is that of the terms, rounded (2^-8), not that of a truncating accumulator (off by 1.4e-2).  64
+    stretches of 4096 terms each lose at most 2^-13 of themselves on average, the sums behind are to nearest."""
+    torch = _torch()
+    rows, n = 1 << 27, 8
+    g = gen(3)
+    x, dy = ((torch.rand(rows, n, generator=g, device="cuda") * 0.5 + 0.5).bfloat16() for _ in range(2))
+    dw, db = torch.empty(n, n, device="cuda", dtype=torch.bfloat16), torch.empty(n, device="cuda", dtype=torch.bfloat16)
+    gpu.linear_grad(dy, x, torch.zeros(n, n, device="cuda", dtype=torch.bfloat16), None, None, dw, db)
+    want, total = torch.zeros(n, n, dtype=torch.float64, device="cuda"), torch.zeros(n, dtype=torch.float64, device="cuda")
+    for i in range(0, rows, 1 << 22):
+        part = dy[i:i + (1 << 22)].double()
+        want += x[i:i + (1 << 22)].double().T @ part
+        total += part.sum(0)
+    within(dw, want, (2.0 ** -8 + 2.0 ** -12) * want)
+    within(db, total, (2.0 ** -8 + 2.0 ** -12) * total)
+
+
+@pytest.mark.parametrize("K", [65536, 65600, 131072])
+def test_linear_bf16_long_sums_do_not_drift(K):
+    """Terms of one sign, tiles enough that no sum is split: the mean error, in which the roundings to bf16 cancel, stays below an eighth of one."""
+    torch = _torch()
+    M, N = 2500, 2560
+    g = gen(K)
+    x = torch.empty(M, K, device="cuda", dtype=torch.bfloat16).uniform_(0.5, 1.5, generator=g)
+    w = torch.empty(K, N, device="cuda", dtype=torch.bfloat16).uniform_(0.5, 1.5, generator=g)
+    b, r = randn(g, N, scale=1e4, dtype=torch.bfloat16), randn(g, M, N, scale=1e4, dtype=torch.bfloat16)
+    y, z = torch.empty(M, N, device="cuda", dtype=torch.bfloat16), torch.empty(M, N, device="cuda", dtype=torch.bfloat16)
+    gpu.linear(x, w, b, r, y, pre=z)
+    want = torch.zeros(M, N, dtype=torch.float64, device="cuda")
+    for k in range(0, K, 16384):
+        want += x[:, k:k + 16384].double() @ w[k:k + 16384].double()
+    total = want.clone()                                 # (of K positive terms; bias and residual can turn the results' sign)
+    for got, more in ((z, b.double()), (y, r.double())):
+        want += more
+        assert abs(float((got.double() - want).mean())) <= 2.0 ** -11 * float(total.mean())
+        within(got, want, 2.0 ** -8 * want.abs() + 2.0 ** -10 * total)
+
+
 def test_linear_fp32_of_what_pieces_cannot_hold():
     """Infinities, NaN, the largest and the smallest numbers: the results of fp32 all the same, in the forward and the backward products."""
     torch = _torch()

@@ -209,3 +209,12 @@ def test_the_bound_of_products_in_pieces_sees_each_pair():
     assert np.all(np.abs(total - want) <= 2.0 ** -23 * np.abs(want))
     for p in PAIRS:
         assert np.mean(np.abs(total - terms[p] - want) > 2.0 ** -22 * np.abs(want)) > 0.8
+
+
+def test_long_sums_leave_the_tensor_cores_in_stretches():
+    """A weight gradient over 16.5 million rows has 64 tiles for 74 pairs of CTAs, each a sum of 0.1 s in one go, as long as a kernel waits for anything:
+    it needs room for fp32 sums outside tensor memory.  Those of a dataset of 60000 rows do not."""
+    for rows, n in ((16_500_000, 2048), (5_000_000, 4096), (3_200_000, 8192)):
+        assert gpu.linear_scratch_bytes(rows, n, n, gpu.ACT_NONE, gpu.BF16_FP32MASTER, True, 7) >= 4 * n * n
+    for rows, n in ((60000, 4096), (8192, 4096)):
+        assert gpu.linear_scratch_bytes(rows, n, n, gpu.ACT_NONE, gpu.BF16_FP32MASTER, True, 7) < 4 * n * n
