@@ -34,10 +34,10 @@ constexpr int THREADS = 64 + 32 * EPI_WARPS;
 // terms of one sign was off by 9.7e-5.  So products of pieces add up there over a stretch of blocks only; the epilogue's warps take each stretch out
 // and add it in registers, rounding to nearest, while the next one runs.  SMALL_STRETCH in the passes of the smaller pairs, whose steps count 2^-7 and
 // less, STRETCH in the last pass: with 8, 4 or 2 blocks that product is off by 2.6e-7, 1.4e-7 or 2.0e-7 (one of both signs by 4.9e-7, 2.8e-7 or 2.6e-7
-// of its size; on FP32 FMAs 1.1e-6 and 1.8e-6) and takes (2048 x 20000 x 1024) 470, 490 or 515 us, 476 in one stretch.
+// of its size; on FP32 FMAs 1.1e-6 and 1.8e-6) and takes (2048 x 20000 x 1024) 470, 490 or 515 us, 460 in one stretch.
 // A sum in bf16 is rounded by up to 2^-8 and left in one stretch up to LONG_SUM blocks (65536 terms of one sign: off by 4e-4); longer ones go in
 // stretches of LONG_STRETCH (off by 8e-6; 134 million terms 1.4e-2 before), which also keeps the epilogue's wait for a stretch below half a millisecond.
-constexpr int SMALL_STRETCH = 64, STRETCH = 4, LONG_SUM = 1024, LONG_STRETCH = 64;
+constexpr int SMALL_STRETCH = 64, STRETCH = 4, LONG_SUM = 1024, LONG_STRETCH = 64;      // (stretches: powers of two)
 
 struct Args {
   int a_mn, b_mn;                        // operand layouts: 0 K-major, 1 MN-major
@@ -119,8 +119,8 @@ __device__ __forceinline__ void box_rows_out(const uint8_t* box, int lane, __nv_
 // First block behind the stretch that starts with block kb, of a tile's blocks in front of `end`.
 __device__ __forceinline__ int stretch_end(const Args& p, int kb, int end) {
   const int small = p.n_kb - p.kb_pass;
-  if (kb < small) return min(min((kb / SMALL_STRETCH + 1) * SMALL_STRETCH, small), end);
-  return min(small + ((kb - small) / p.stretch + 1) * p.stretch, end);
+  if (kb < small) return min(min(kb + SMALL_STRETCH - (kb & (SMALL_STRETCH - 1)), small), end);
+  return min(kb + p.stretch - ((kb - small) & (p.stretch - 1)), end);
 }
 
 // STRETCHES: sums that leave tensor memory in stretches, partial results: fp32 operands in pieces, long sums in bf16; an own instance, since the
@@ -332,6 +332,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
       const int row0 = c.i0 + q * 32, row = row0 + lane;
       if constexpr (STRETCHES) {
         const int j0 = c.j0 + half * HALF_COLS;
+        constexpr int LD = HALF_COLS < 128 ? 64 : 32;      // (columns under way: 168 registers)
         uint32_t sum[HALF_COLS];               // (binary32)
 #pragma unroll
         for (int i = 0; i < HALF_COLS; ++i) sum[i] = 0u;
@@ -344,12 +345,13 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
           if (works && row0 < p.I) {           // (uniform in the warp)
             const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN + half * HALF_COLS);
 #pragma unroll
-            for (int c0 = 0; c0 < HALF_COLS; c0 += 32)
+            for (int c0 = 0; c0 < HALF_COLS; c0 += LD)
               if (j0 + c0 < p.J) {
-                uint32_t v[32];
-                tmem_ld32(t_row + (uint32_t)c0, v);
+                uint32_t v[LD];
+                if constexpr (LD == 64) tmem_ld64(t_row + (uint32_t)c0, v);
+                else tmem_ld32(t_row + (uint32_t)c0, v);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) sum[c0 + i] = __float_as_uint(__uint_as_float(sum[c0 + i]) + __uint_as_float(v[i]));
+                for (int i = 0; i < LD; ++i) sum[c0 + i] = __float_as_uint(__uint_as_float(sum[c0 + i]) + __uint_as_float(v[i]));
               }
           }
           release();
