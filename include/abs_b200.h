@@ -372,8 +372,10 @@ int abs_group_norm_scratch_bytes(long long samples, long long positions, int cha
                                  size_t* out);
 
 /* Status of the layer operations on the current device: ABS_ETIMEOUT if, since the last call of this
- * function, a bounded wait (100 ms) inside one of their kernels ran out, whose results are then not valid; else
- * ABS_OK.  Synchronises the stream; operations on other streams are covered once they have completed. */
+ * function on that device by any thread, a bounded wait (100 ms) inside one of their kernels ran out, whose
+ * results are then not valid; else ABS_OK.  Synchronises the stream; operations on other streams are covered
+ * once they have completed.  The operations themselves return before their kernels run: whoever needs their
+ * results to be certain asks here before using them. */
 int abs_op_status(void* stream);
 
 /* Test aid for that path: enqueues a one-warp kernel that waits, with these kernels' own wait routine and a limit of

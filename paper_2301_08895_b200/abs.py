@@ -571,11 +571,13 @@ def group_norm_grad(dy, x, groups, w, b, mean, rstd, dx, dw, db, act=ACT_NONE, s
 
 
 def op_status(stream=None):
-    """abs_op_status on the current device: waits for `stream` (default: the current one) and raises AbsError(ETIMEOUT) if a
-    bounded wait of a layer operation ran out since the last call."""
+    """abs_op_status on the device of `stream` (default: the current one): waits for the stream and raises AbsError(ETIMEOUT) if a bounded wait of a
+    layer operation on that device ran out since the last call.  The operations do not wait for their own results: a program asks before it
+    relies on them, once per step or evaluation.  One report per device, whichever thread asks first."""
     import torch
     s = stream if stream is not None else torch.cuda.current_stream()
-    _check(lib().abs_op_status(s.cuda_stream))
+    with torch.cuda.device(s.device):
+        _check(lib().abs_op_status(s.cuda_stream))
 
 
 def trace_rows(tr):

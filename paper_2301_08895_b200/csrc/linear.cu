@@ -341,10 +341,11 @@ cudaError_t launch_tile(const Plan& pl, const CUtensorMap& a, const CUtensorMap&
          : pl.bn == 128 ? launch_dense<128, 1, STRETCHES>(a, b, o, z, p, sms, device, s) : launch_dense<64, 1, STRETCHES>(a, b, o, z, p, sms, device, s);
 }
 
-__device__ int g_status;                 // set by a kernel whose bounded wait ran out; read and cleared by abs_op_status
-int* status_word(int device) {
-  static std::atomic<int*> known[MAX_DEVICES];
-  int* p = known[device].load(std::memory_order_acquire);
+__device__ unsigned g_status;            // how often a CTA's bounded wait ran out: only ever counted up, so that no report is lost to a reader
+std::atomic<unsigned> g_status_seen[MAX_DEVICES];      // what abs_op_status has reported of it
+unsigned* status_word(int device) {
+  static std::atomic<unsigned*> known[MAX_DEVICES];
+  unsigned* p = known[device].load(std::memory_order_acquire);
   if (!p && cudaGetSymbolAddress((void**)&p, g_status) == cudaSuccess) known[device].store(p, std::memory_order_release);
   return p;
 }
@@ -917,7 +918,7 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
 
 // One warp waits for an arrival that never comes, as the kernels of these operations wait, and reports it as they do.
 namespace {
-__global__ void op_wait_selftest_kernel(int* status, unsigned long long limit_ns) {
+__global__ void op_wait_selftest_kernel(unsigned* status, unsigned long long limit_ns) {
   __shared__ uint64_t bar;
   __shared__ int gave_up;
   grid_dependency_sync();
@@ -927,7 +928,7 @@ __global__ void op_wait_selftest_kernel(int* status, unsigned long long limit_ns
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
-  if (threadIdx.x == 0 && !tc::mbar_wait(&bar, 0u, &gave_up, limit_ns)) *status = 1;
+  if (threadIdx.x == 0 && !tc::mbar_wait(&bar, 0u, &gave_up, limit_ns)) atomicAdd(status, 1u);
 }
 }  // namespace
 
@@ -936,21 +937,23 @@ extern "C" int abs_op_selftest_wait_timeout(int limit_us, void* stream) {
   int device, sms;
   const int rc = current_device(&device, &sms);
   if (rc != ABS_OK) return rc;
-  int* word = status_word(device);
+  unsigned* word = status_word(device);
   if (!word) return fail(ABS_ECUDA, "cudaGetSymbolAddress(status) failed");
   const cudaError_t e = launch(op_wait_selftest_kernel, dim3(1), 32, 0, 1, (cudaStream_t)stream, word, 1000ull * (unsigned long long)limit_us);
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }
 
 extern "C" int abs_op_status(void* stream) {
-  int device, sms, v = 0;
+  int device, sms;
   const int rc = current_device(&device, &sms);
   if (rc != ABS_OK) return rc;
-  int* word = status_word(device);
+  unsigned* word = status_word(device);
   if (!word) return fail(ABS_ECUDA, "cudaGetSymbolAddress(status) failed");
+  unsigned v = 0;
   cudaError_t e = cudaMemcpyAsync(&v, word, sizeof v, cudaMemcpyDeviceToHost, (cudaStream_t)stream);
   if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
-  if (e == cudaSuccess && v) e = cudaMemsetAsync(word, 0, sizeof v, (cudaStream_t)stream);
   if (e != cudaSuccess) return fail(ABS_ECUDA, "status: %s", cudaGetErrorString(e));
-  return v ? fail(ABS_ETIMEOUT, "a bounded wait in a layer operation ran out: its results are not valid") : ABS_OK;
+  unsigned seen = g_status_seen[device].load();
+  while ((int)(v - seen) > 0 && !g_status_seen[device].compare_exchange_weak(seen, v)) {}
+  return (int)(v - seen) > 0 ? fail(ABS_ETIMEOUT, "a bounded wait in a layer operation ran out: its results are not valid") : ABS_OK;
 }

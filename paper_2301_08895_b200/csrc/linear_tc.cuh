@@ -16,7 +16,7 @@
 // rows x 128 bytes per warp in shared memory, one bulk store per box.  CG = 2: a cluster of two CTAs shares a tile of 256 x BN,
 // each loads its own rows of A and half of B.  A sum can be split over `splits` tiles that leave fp32 partial results, and products of pieces leave
 // tensor memory in stretches (below).
-// Every wait is bounded: on expiry the CTA raises the operations' status word, drains its copies, frees tensor memory and returns.
+// Every wait is bounded: on expiry the CTA counts up the operations' status word, drains its copies, frees tensor memory and returns.
 #pragma once
 #include "layerops.cuh"
 #include "linear_split.cuh"
@@ -51,7 +51,7 @@ struct Args {
   long long ldr, ldo, ldp;
   int act, out_tma, pre_tma, res_vec, bias_vec;   // stores by TMA; residual rows, bias on 16-byte boundaries
   int partial;                           // 1: fp32 partial results through map_out instead
-  int* status;
+  unsigned* status;                      // counts CTAs whose wait ran out
 };
 
 template <int BN, int CG> struct Cfg {
@@ -475,7 +475,7 @@ dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(C::TMEM_COLS) : "memory");
     else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(C::TMEM_COLS) : "memory");
   }
-  if (threadIdx.x == 0 && *abort) *p.status = 1;
+  if (threadIdx.x == 0 && *abort) atomicAdd(p.status, 1u);
 }
 
 }  // namespace dense

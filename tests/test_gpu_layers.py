@@ -6,6 +6,7 @@ terms in fp32 that may truncate (2^-23 of the sum of magnitudes per addition), a
 2^-20 at the arguments used, slopes |act'| <= 1.13 and |act''| <= 0.8.
 """
 import math
+import time
 
 import numpy as np
 import pytest
@@ -1201,6 +1202,48 @@ def test_a_wait_that_runs_out_is_reported_once():
     assert e.value.code == gpu.ETIMEOUT
     gpu.op_status()
     test_linear_adds_to_the_residual_in_place(True)               # (the operations go on working)
+    gpu.op_status()
+
+
+def test_no_report_of_a_wait_is_lost_beside_other_readers():
+    """Two threads ask for the status all the time while waits run out on a third stream, one at a time: one of them, or the last question, reports
+    each."""
+    import threading
+    torch = _torch()
+    gpu.op_status()
+    reports, done, lock = [0], threading.Event(), threading.Lock()
+
+    def ask(stream):
+        try:
+            gpu.op_status(stream)
+        except gpu.AbsError as e:
+            assert e.code == gpu.ETIMEOUT
+            with lock:
+                reports[0] += 1
+
+    def reader():
+        stream = torch.cuda.Stream()
+        while not done.is_set():
+            ask(stream)
+    threads = [threading.Thread(target=reader) for _ in range(2)]
+    for t in threads:
+        t.start()
+    raised = torch.cuda.Stream()
+    lost = 0
+    for k in range(300):
+        before = reports[0]
+        assert gpu.lib().abs_op_selftest_wait_timeout(1 + k % 7, raised.cuda_stream) == gpu.OK
+        raised.synchronize()
+        ask(raised)
+        for _ in range(2000):
+            if reports[0] > before:
+                break
+            time.sleep(1e-4)
+        lost += reports[0] == before
+    done.set()
+    for t in threads:
+        t.join()
+    assert lost == 0 and reports[0] == 300
     gpu.op_status()
 
 
