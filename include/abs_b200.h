@@ -290,8 +290,9 @@ int abs_lsq_gradient_noalloc(const void* X, const float* y, const void* w, const
  *    where it is stored, unless a function says otherwise.  Larger ABS_FP32 matrix products run on
  *    the tensor cores from three bf16 numbers per element, whose sum is the element: a product of two
  *    elements is then off by at most 2^-22 of it, a sum of products no more than one formed by fp32
- *    multiply-adds one after the other, and data that cannot be split so (infinities, NaN,
- *    numbers of 2^63 and more or below 2^-110) are multiplied in fp32, slower.
+ *    multiply-adds one after the other, and data whose scaled sums could overflow
+ *    (infinities, NaN, numbers of 2^42 and more with 1024 terms, 2^37 with 2^20) are multiplied in fp32,
+ *    slower.
  *  - Matrices are row-major device memory with a row pitch (ld*, in elements, at least the number
  *    of columns); what lies between the rows and behind the last one is neither read nor written.
  *    Any alignment of the stored type is accepted.

@@ -569,8 +569,12 @@ split3::Matrix in_pieces(const void* src, long long ld, long long rows, int cols
   m.per_row = Divisor((uint32_t)(m.cols_p / 8));
   return m;
 }
-cudaError_t split(std::initializer_list<split3::Matrix> ms, Flags* flags, cudaStream_t s) {
+// terms: of the longest sum over these matrices
+cudaError_t split(std::initializer_list<split3::Matrix> ms, long long terms, Flags* flags, cudaStream_t s) {
   split3::Args a = {};
+  int log_terms = 0;
+  while ((1ll << log_terms) < terms) ++log_terms;
+  a.limit = ldexpf(1.f, (94 - log_terms) / 2);
   uint32_t n = 0, i = 0;
   for (const split3::Matrix& m : ms) {
     a.m[i] = m;
@@ -785,7 +789,7 @@ extern "C" int abs_linear(const void* x, long long ldx, const void* w, long long
       char* sc = (char*)scratch;
       Flags flags = {(uint32_t*)(sc + f.flags), 0};
       const split3::Matrix mx = in_pieces(x, ldx, rows, n_in, sc), mw = in_pieces(w, ldw, n_in, n_out, sc + f.w);
-      const cudaError_t e = split({mx, mw}, &flags, s);
+      const cudaError_t e = split({mx, mw}, n_in, &flags, s);
       if (e != cudaSuccess) return fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
       return pieces_product(mx, 0, mw, 1, p, f.tc, (int)rows, n_out, n_in, act, flags, (float*)(sc + f.part), sms, device, s);
     }
@@ -871,7 +875,8 @@ extern "C" int abs_linear_grad(const void* dy, long long lddy, const void* x, lo
     const split3::Matrix mw = dx ? in_pieces(w, ldw, n_in, n_out, sc + g.pw) : none;
     Flags flags = {(uint32_t*)(sc + g.flags), 0};
     if (g.pieces && (dx || dw)) {
-      e = dx && dw ? split({mz, mx, mw}, &flags, s) : dw ? split({mz, mx}, &flags, s) : split({mz, mw}, &flags, s);
+      const long long terms = dw && (rows > n_out || !dx) ? rows : n_out;
+      e = dx && dw ? split({mz, mx, mw}, terms, &flags, s) : dw ? split({mz, mx}, terms, &flags, s) : split({mz, mw}, terms, &flags, s);
       if (e != cudaSuccess) return fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
     }
     fp32::Args px = {}, pw = {};

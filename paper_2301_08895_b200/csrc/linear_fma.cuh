@@ -158,7 +158,8 @@ template <int BN, int ACT> __device__ __noinline__ void finish_tile(const Args& 
       const int r = r0 + u * hop;
       if (r >= X) continue;
       const long long i = i0 + r;
-      const float v[4] = {z[u].x + bias[0], z[u].y + bias[1], z[u].z + bias[2], z[u].w + bias[3]};
+      const float v[4] = {fmaf(z[u].x, split3::DOWN, bias[0]), fmaf(z[u].y, split3::DOWN, bias[1]), fmaf(z[u].z, split3::DOWN, bias[2]),
+                          fmaf(z[u].w, split3::DOWN, bias[3])};
       const float y[4] = {layer::act_value<ACT>(v[0]) + res[u].x, layer::act_value<ACT>(v[1]) + res[u].y, layer::act_value<ACT>(v[2]) + res[u].z,
                           layer::act_value<ACT>(v[3]) + res[u].w};
       float* out = p.out + i * p.ldo + j;

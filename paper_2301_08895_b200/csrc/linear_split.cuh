@@ -6,9 +6,10 @@
 // the other, the smallest first, so that only the last pass adds to sums of the result's size; its own additions are linear_tc.cuh's, 256 terms
 // at a time.  The whole sum is off by less than fused multiply-adds one after the other (4096 terms of both signs: 2.4e-7 of its size for 8.1e-7).
 //
-// Exactness needs pieces that bf16 can hold: infinities, NaN and elements other than zero below 2^-110 raise their block's flag, so do elements
-// of 2^63 and more, whose rounded pieces could overflow where the product does not.  The product is then taken from the fp32 matrices by
-// fused multiply-adds instead: the results are fp32's whatever the data, and the cost of such data is time (4096^3: 2.5 ms for 0.65).
+// Pieces are those of 2^16 a, so that all 24 bits of any small a, denormal ones included, are multiples of 2^-133, bf16's smallest number; the epilogue
+// takes 2^-32 of the sums.  The scaled sums overflow before those of fp32 do: infinities, NaN and elements of 2^L and more, 2 L = 94 - log2 of the terms
+// (rounded up), raise their block's flag.  The product is then taken from the fp32 matrices by fused multiply-adds instead: the results are
+// fp32's whatever the data, and the cost of such data is time (4096^3: 2.5 ms for 0.75).
 //
 // 4096^3 with GELU: splitting 67 us (335 MB, 5 TB/s), products 565 us (1.46 PFLOP/s in bf16), epilogue 40; the plain kernel takes 2507.
 //
@@ -30,7 +31,8 @@ struct Matrix {
   layer::Divisor per_row;                                 // groups of eight columns
   uint32_t end;                                           // groups of this matrix and the ones before it
 };
-struct Args { Matrix m[3]; uint32_t n; uint32_t* flags; };
+struct Args { Matrix m[3]; uint32_t n; uint32_t* flags; float limit; };     // limit: 2^L
+constexpr float UP = 0x1p16f, DOWN = 0x1p-32f;
 
 // Whether any block of the split raised its flag; all threads of the block take part.
 __device__ __forceinline__ bool any_flag(const uint32_t* flags, int n) {
@@ -60,9 +62,10 @@ __global__ void __launch_bounds__(256) split_kernel(const __grid_constant__ Args
     __nv_bfloat16 p[3][8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      p[0][e] = __float2bfloat16_rn(v[e]);
-      const float hi = __bfloat162float(p[0][e]), rest = v[e] - hi;
-      bad |= !(fabsf(hi) < 0x1p63f) || (v[e] != 0.f && fabsf(v[e]) < 0x1p-110f);
+      bad |= !(fabsf(v[e]) < a.limit);
+      const float up = v[e] * UP;
+      p[0][e] = __float2bfloat16_rn(up);
+      const float rest = up - __bfloat162float(p[0][e]);
       p[1][e] = __float2bfloat16_rn(rest);
       p[2][e] = __float2bfloat16_rn(rest - __bfloat162float(p[1][e]));
     }

@@ -470,6 +470,55 @@ def test_linear_fp32_of_what_pieces_cannot_hold():
         within(dw, xx.double().T @ dy.double(), 1.2 * (M + 4) * E23 * (xx.double().abs().T @ dy.double().abs()))
 
 
+def test_linear_fp32_in_pieces_of_tiny_elements():
+    """One element of a saturated unit's size, down to the smallest float, sends nothing to the slow kernel: results that it cannot reach keep their bits.
+    Whole matrices of that size have fp32's results."""
+    torch = _torch()
+    M, K, N = 520, 1024, 1030
+    assert takes_pieces(M, K, N) and takes_pieces(M, K, N, True)
+    g = gen(12)
+    x, w, dy = randn(g, M, K), randn(g, K, N), randn(g, M, N)
+
+    def results():
+        y, dx, dw = torch.empty(M, N, device="cuda"), torch.empty_like(x), torch.empty_like(w)
+        gpu.linear(x, w, None, None, y)
+        gpu.linear_grad(dy, x, w, None, dx, dw, None)
+        return y, dx, dw
+    x[17, 33] = dy[5, 99] = w[40, 21] = 0.0
+    y0, dx0, dw0 = results()
+    for tiny in (2.0 ** -111, 2.0 ** -126, 1e-42, 2.0 ** -149):
+        x[17, 33], dy[5, 99], w[40, 21] = tiny, -tiny, tiny
+        y, dx, dw = results()
+        assert torch.equal(y, y0) and torch.equal(dx, dx0) and torch.equal(dw, dw0)
+    lowest = 2.0 ** -149
+    for down, up in ((2.0 ** -112, 2.0 ** 30), (2.0 ** -128, 2.0 ** 12), (2.0 ** -140, 1.0), (2.0 ** -60, 2.0 ** -75)):
+        a, b, c = randn(g, M, K) * down, randn(g, K, N) * up, randn(g, M, N) * down
+        y, dx, dw = torch.empty(M, N, device="cuda"), torch.empty_like(a), torch.empty_like(b)
+        gpu.linear(a, b, None, None, y)
+        gpu.linear_grad(c, b[:M, :K].contiguous(), b, None, dx, dw, None)
+        xx = b[:M, :K].double()
+        tol = lambda p, q, n: 1.2 * (n + 4) * E23 * (p.abs() @ q.abs()) + lowest           # noqa: E731
+        within(y, a.double() @ b.double(), tol(a.double(), b.double(), K))
+        within(dx, c.double() @ b.double().T, tol(c.double(), b.double().T, N))
+        within(dw, xx.T @ c.double(), tol(xx.T, c.double(), M))
+
+
+@pytest.mark.parametrize("size", [41.9, 42.5, 58.0])
+def test_linear_fp32_in_pieces_of_large_elements(size):
+    """Terms of one sign up to where scaled sums would overflow, and beyond: fp32's sums, which do not."""
+    torch = _torch()
+    M, K, N = 520, 1024, 1030
+    assert takes_pieces(M, K, N) and takes_pieces(M, K, N, True)
+    x, w, dy = (torch.full(s, 2.0 ** size, device="cuda") for s in ((M, K), (K, N), (M, N)))
+    y, dx, dw = torch.empty(M, N, device="cuda"), torch.empty(M, K, device="cuda"), torch.empty(K, N, device="cuda")
+    gpu.linear(x, w, None, None, y)
+    gpu.linear_grad(dy, x, w, None, dx, dw, None)
+    square = float(x[0, 0]) ** 2
+    for got, n in ((y, K), (dx, N), (dw, M)):
+        want = torch.full_like(got, n * square, dtype=torch.float64)
+        within(got, want, (n + 4) * 2.0 ** -24 * want)
+
+
 def test_linear_fp32_in_pieces_captured_and_on_another_stream():
     """The flags of a step are its own: a replay with an infinity in x, and one without it again."""
     torch = _torch()
