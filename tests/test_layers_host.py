@@ -218,3 +218,19 @@ def test_long_sums_leave_the_tensor_cores_in_stretches():
         assert gpu.linear_scratch_bytes(rows, n, n, gpu.ACT_NONE, gpu.BF16_FP32MASTER, True, 7) >= 4 * n * n
     for rows, n in ((60000, 4096), (8192, 4096)):
         assert gpu.linear_scratch_bytes(rows, n, n, gpu.ACT_NONE, gpu.BF16_FP32MASTER, True, 7) < 4 * n * n
+
+
+def test_scratch_of_no_rows_and_of_every_alignment():
+    """No rows need none; the query without known alignments covers all of them."""
+    for dtype in (gpu.FP32, gpu.BF16_FP32MASTER):
+        for grad in (False, True):
+            for act in (gpu.ACT_NONE, gpu.ACT_GELU):
+                for aligned in range(8):
+                    for n_in, n_out in ((8, 8), (1, 1), (785, 10), (4096, 4096)):
+                        assert gpu.linear_scratch_bytes(0, n_in, n_out, act, dtype, grad, aligned) == 0
+                for rows, n_in, n_out in ((1, 1, 1), (2, 9, 9), (9, 4096, 64), (300, 256, 10), (1000, 785, 10), (60000, 784, 256), (8192, 4096, 4096),
+                                          (1 << 27, 8, 8), (16_500_000, 2048, 2048)):
+                    every = [gpu.linear_scratch_bytes(rows, n_in, n_out, act, dtype, grad, aligned) for aligned in range(8)]
+                    assert every[0] == max(every), (rows, n_in, n_out, act, dtype, grad, every)
+            for samples, positions in ((0, 5), (5, 0), (0, 0)):
+                assert gpu.group_norm_scratch_bytes(samples, positions, 6, 3, dtype, grad) == 0
