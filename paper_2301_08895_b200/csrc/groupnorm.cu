@@ -1127,6 +1127,17 @@ Span maps_span(const void* ptr, long long s, long long p, long long samples, lon
   return r;
 }
 
+// Two maps of one shape share a byte.  With equal pitches they do not if each position of the one lies in the gap behind (in front of) that of the
+// other, as channel ranges of one buffer do.
+struct Maps { const void* p; long long s, i; Span span; };        // pitches of samples and positions
+bool maps_overlap(const Maps& a, const Maps& b, long long samples, long long positions, int C, size_t esz) {
+  if (!overlap(a.span, b.span)) return false;
+  if ((samples > 1 && a.s != b.s) || (positions > 1 && a.i != b.i)) return true;
+  const unsigned long long row = C * (unsigned long long)esz, pitch = a.i * (unsigned long long)esz, sample = a.s * (unsigned long long)esz;
+  const unsigned long long d = (uintptr_t)a.p < (uintptr_t)b.p ? (uintptr_t)b.p - (uintptr_t)a.p : (uintptr_t)a.p - (uintptr_t)b.p;
+  return d < row || (positions > 1 && d + row > pitch) || (samples > 1 && (positions - 1) * pitch + d + row > sample);
+}
+
 }  // namespace
 
 extern "C" int abs_group_norm_scratch_bytes(long long samples, long long positions, int channels, int groups, int dtype, int grad,
@@ -1155,7 +1166,7 @@ extern "C" int abs_group_norm(const void* x, long long xs, long long xp, const v
   if ((rc = check_vector("mean", mean, 4)) != ABS_OK || (rc = check_vector("rstd", rstd, 4)) != ABS_OK) return rc;
   const Span sx = maps_span(x, xs, xp, samples, positions, channels, esz), sy = maps_span(y, ys, yp, samples, positions, channels, esz);
   const Span sw = flat(w, channels * esz), sb = flat(b, channels * esz), sm = flat(mean, samples * groups * 4), sr = flat(rstd, samples * groups * 4);
-  if (!(x == y && (samples == 1 || xs == ys) && (positions == 1 || xp == yp)) && overlap(sx, sy)) return fail(ABS_EINVAL, "y overlaps x without being the same maps");
+  if (!(x == y && (samples == 1 || xs == ys) && (positions == 1 || xp == yp)) && maps_overlap({x, xs, xp, sx}, {y, ys, yp, sy}, samples, positions, channels, esz)) return fail(ABS_EINVAL, "y overlaps x without being the same maps");
   if (overlap(sy, sw) || overlap(sy, sb)) return fail(ABS_EINVAL, "y overlaps w or b");
   if (overlap(sm, sr)) return fail(ABS_EINVAL, "mean overlaps rstd");
   for (const Span& st : {sm, sr})
@@ -1206,8 +1217,9 @@ extern "C" int abs_group_norm_grad(const void* dy, long long dys, long long dyp,
   const Span sx = maps_span(x, xs, xp, samples, positions, channels, esz), sg = maps_span(dy, dys, dyp, samples, positions, channels, esz);
   const Span sd = maps_span(dx, dxs, dxp, dx ? samples : 0, positions, channels, esz), s1 = flat(dw, channels * esz), s2 = flat(db, channels * esz);
   const Span fixed[4] = {flat(w, channels * esz), flat(b, channels * esz), flat(mean, samples * groups * 4), flat(rstd, samples * groups * 4)};
-  if (overlap(sd, sx)) return fail(ABS_EINVAL, "dx overlaps x");
-  if (!(dx == dy && (samples == 1 || dxs == dys) && (positions == 1 || dxp == dyp)) && overlap(sd, sg))
+  const Maps mx = {x, xs, xp, sx}, mg = {dy, dys, dyp, sg}, md = {dx, dxs, dxp, sd};
+  if (maps_overlap(md, mx, samples, positions, channels, esz)) return fail(ABS_EINVAL, "dx overlaps x");
+  if (!(dx == dy && (samples == 1 || dxs == dys) && (positions == 1 || dxp == dyp)) && maps_overlap(md, mg, samples, positions, channels, esz))
     return fail(ABS_EINVAL, "dx overlaps dy without being the same maps");
   if (overlap(s1, s2) || overlap(s1, sd) || overlap(s2, sd)) return fail(ABS_EINVAL, "two gradients overlap");
   for (const Span& o : {sd, s1, s2})

@@ -1419,3 +1419,32 @@ def test_gelu_on_a_dense_grid():
     gpu.group_norm_grad(dy, x, 1, None, z, mean, rstd, None, None, db2, gpu.ACT_GELU)
     for d in (db, db2):
         within(d, slope, torch.full_like(slope, 2.0 ** -20))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("P,pad", [(1, 0), (1, 5), (9, 0), (9, 3)])
+def test_group_norm_of_channel_ranges_of_one_buffer(P, pad, bf16):
+    """Maps that are channel ranges of one buffer do not overlap: also with one position per sample, and where a sample's pitch is no multiple of a
+    position's.  One channel less between them and they do."""
+    torch = _torch()
+    d, C, N = dt(bf16), 16, 6
+    wide = 3 * C + 8
+    buf = torch.full((N * (P * wide + pad) + 16,), 7.0, device="cuda", dtype=d)
+    part = lambda c: buf.as_strided((N, P, C), (P * wide + pad, wide, 1), c)         # noqa: E731
+    x, y, dx = part(0), part(C + 8), part(2 * C + 8)
+    x.copy_(randn(gen(P), N, P, C, dtype=d))
+    keep = x.clone()
+    mean, rstd, want = torch.empty(N, 2, device="cuda"), torch.empty(N, 2, device="cuda"), torch.empty_like(keep)
+    gpu.group_norm(keep, 2, None, None, want, mean, rstd, 1e-5, gpu.ACT_GELU)
+    gpu.group_norm(x, 2, None, None, y, None, None, 1e-5, gpu.ACT_GELU)
+    assert torch.equal(y, want) and torch.equal(x, keep)
+    dy = randn(gen(P + 1), N, P, C, dtype=d)
+    y.copy_(dy)
+    gpu.group_norm_grad(dy, keep, 2, None, None, mean, rstd, want, None, None, gpu.ACT_GELU)
+    gpu.group_norm_grad(y, x, 2, None, None, mean, rstd, dx, None, None, gpu.ACT_GELU)
+    assert torch.equal(dx, want) and torch.equal(y, dy) and torch.equal(x, keep)
+    assert bool((part(C)[:, :, :8] == 7.0).all())
+    for other in (part(C - 1), part(2 * C + 9 + (pad if P == 1 else 0))):  # (the last one's end reaches the next position's first channel)
+        with pytest.raises(gpu.AbsError) as e:
+            gpu.group_norm(x[:N - 1], 2, None, None, other[:N - 1], None, None)
+        assert e.value.code == gpu.EINVAL
