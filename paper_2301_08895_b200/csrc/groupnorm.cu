@@ -1,4 +1,5 @@
 // Group normalisation of channels-last maps with an activation, and its gradients.
+#include <algorithm>
 #include <atomic>
 
 #include "layerops.cuh"
@@ -986,13 +987,18 @@ Plan plan(long long samples, long long positions, int C, int G, int dtype, bool 
   p.R = SNT / (p.cw / VE);
   // ranges of positions: as many as keep the waves of CTAs (three per SM) short, a CTA costing about as much as 12 rows
   // besides its own
-  const long long units = samples * p.blocks, most_parts = (positions + 8 * p.R - 1) / (8 * p.R), slots = 3 * PLAN_SMS;
+  const long long units = samples * p.blocks, slots = 3 * PLAN_SMS;
+  const long long most_parts = std::min({(positions + 8 * p.R - 1) / (8 * p.R), 4096ll, 12 * PLAN_SMS / units + 1});
   long long parts = 1;
   double least = 1e300;
-  for (long long n = 1; n <= most_parts && n <= 4096 && (n - 1) * units <= 12 * PLAN_SMS; ++n) {
-    const long long ppc = (positions + n - 1) / n;
-    const double cost = (double)((n * units + slots - 1) / slots) * (double)((ppc + p.R - 1) / p.R + 12);
-    if (cost < least) { least = cost; parts = n; }
+  // among the numbers of ranges with as many waves the largest has the fewest rows; the smallest with as few rows is as good
+  for (long long waves = (units + slots - 1) / slots, last = 0; last < most_parts; ++waves) {
+    const long long n = std::min(most_parts, waves * slots / units);
+    if (n == last) continue;                                     // (a wave too many for the units, and too few for another range)
+    const long long rows = ((positions + n - 1) / n + p.R - 1) / p.R, few = (positions + rows * p.R - 1) / (rows * p.R);
+    const double cost = (double)waves * (double)(rows + 12);
+    if (cost < least) { least = cost; parts = std::max(few, last + 1); }
+    last = n;
   }
   p.sppc = (int)((positions + parts - 1) / parts);
   p.parts = (int)((positions + p.sppc - 1) / p.sppc);

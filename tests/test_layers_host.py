@@ -3,6 +3,7 @@ import ctypes as C
 import os
 import subprocess
 import sys
+import time
 
 import numpy as np
 import pytest
@@ -234,3 +235,15 @@ def test_scratch_of_no_rows_and_of_every_alignment():
                     assert every[0] == max(every), (rows, n_in, n_out, act, dtype, grad, every)
             for samples, positions in ((0, 5), (5, 0), (0, 0)):
                 assert gpu.group_norm_scratch_bytes(samples, positions, 6, 3, dtype, grad) == 0
+
+
+def test_planning_a_few_large_maps_is_quick():
+    """The plan of a call is made on the host each time: for one sample of 512 x 512 x 128 as quickly as for many (two plans of 15 us when every number of
+    ranges was tried, 2 us or less in all)."""
+    f, out = gpu.lib().abs_group_norm_scratch_bytes, C.c_size_t(0)
+    best = 1.0
+    for _ in range(300):
+        t0 = time.perf_counter()
+        f(1, 262144, 128, 32, gpu.BF16_FP32MASTER, 1, C.byref(out))
+        best = min(best, time.perf_counter() - t0)
+    assert out.value > 0 and best < 12e-6
