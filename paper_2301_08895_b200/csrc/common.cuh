@@ -164,4 +164,12 @@ __device__ __forceinline__ float sa_slot_weight(const DevState* st, int t, int s
 __host__ __device__ inline int round_up(int a, int b) { return (a + b - 1) / b * b; }
 __host__ __device__ inline size_t round_up_sz(size_t a, size_t b) { return (a + b - 1) / b * b; }
 
+__device__ __forceinline__ float ld_peer(const float* p, int rank) {       // *p of CTA `rank` of the cluster
+  uint32_t a = (uint32_t)__cvta_generic_to_shared(p), r;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(r) : "memory");
+  return v;
+}
+
 }  // namespace absb

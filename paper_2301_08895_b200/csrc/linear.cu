@@ -625,7 +625,7 @@ int few_rows(const small::Args& a, int dtype, cudaStream_t s) {
   const RowsFn fn = dtype == ABS_FP32 ? (vec ? few_rows_fn<float, 4>(a.rows, a.act) : few_rows_fn<float, 1>(a.rows, a.act))
                                       : (vec ? few_rows_fn<__nv_bfloat16, 8>(a.rows, a.act) : few_rows_fn<__nv_bfloat16, 1>(a.rows, a.act));
   const int M = a.rows <= 2 ? (int)a.rows : a.rows <= 4 ? 4 : 8;
-  const size_t smem = (size_t)(small::NT / 32) * M * (VE << log_l) * 4;          // (at most 32 KB)
+  const size_t smem = (size_t)(small::NT / 32) * M * (VE << log_l) * 4;          // (at most 16 KB)
   const cudaError_t e = launch(fn, dim3(blocks), small::NT, smem, 1, s, a, log_l);
   return e == cudaSuccess ? ABS_OK : fail(ABS_ECUDA, "kernel launch: %s", cudaGetErrorString(e));
 }

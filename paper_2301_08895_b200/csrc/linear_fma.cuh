@@ -43,14 +43,6 @@ template <int BM, int BN> struct Cfg {
   static constexpr size_t SMEM = (size_t)(RING > PARTS ? RING : PARTS) * 4;
 };
 
-__device__ __forceinline__ float ld_peer(const float* p, int rank) {
-  uint32_t a = (uint32_t)__cvta_generic_to_shared(p), r;
-  float v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(r) : "memory");
-  return v;
-}
-
 // Shared memory holds element (k, x) of an operand at [k][x ^ swizzle(k)]: where the sum index is contiguous in memory, a warp copies 32 k
 // of one x (whole lines), and would hit the same eight banks four times over.  Neighbouring pairs of B's columns stay pairs.
 __host__ __device__ constexpr int swizzle_a(int k) { return k >> 3; }

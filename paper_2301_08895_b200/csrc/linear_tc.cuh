@@ -124,7 +124,7 @@ __device__ __forceinline__ int stretch_end(const Args& p, int kb, int end) {
 }
 
 // STRETCHES: sums that leave tensor memory in stretches, partial results: fp32 operands in pieces, long sums in bf16; an own instance, since the
-// bookkeeping costs the other bf16 products 3 % (205 us for 199).
+// bookkeeping costs the other bf16 products 3 % (8192 x 4096 x 4096: 205 us for 199, in turn on one box).
 template <int BN, int CG, bool STRETCHES>
 __global__ void __launch_bounds__(THREADS, 1)
 dense_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
