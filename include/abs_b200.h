@@ -326,7 +326,8 @@ int abs_linear(const void* x, long long ldx, const void* w, long long ldw, const
 /* Gradients of the affine layer: with dz = dy * act'(pre) (pre may be NULL for ABS_ACT_NONE),
  * dx = dz W^T, dw = x^T dz, db = column sums of dz; each of dx, dw, db may be NULL.  The residual's
  * gradient is dy itself.  With ABS_BF16_FP32MASTER dz is rounded to bf16 where it enters the two
- * matrix products (db sums it unrounded). */
+ * matrix products (db sums it unrounded).  ABS_FP32: row pitches of dy, x and w at most 2^24 if they have
+ * more than one row. */
 int abs_linear_grad(const void* dy, long long lddy, const void* x, long long ldx, const void* w, long long ldw,
                     const void* pre, long long ldp, void* dx, long long lddx, void* dw, long long lddw, void* db,
                     long long rows, int n_in, int n_out, int act, int dtype, void* scratch, size_t scratch_bytes,

@@ -61,7 +61,7 @@ namespace {
 constexpr int BK_TERMS = tc::BK;
 
 // dz = dy act'(pre), rounded to storage, and the column sums of the unrounded dz over each chunk of rows: one pass at HBM's pace
-// (8192 x 4096 bf16 GELU: 201 MB in 40 us).  A thread takes VE columns of every R-th row, eight rows' loads under way.
+// (8192 x 4096 bf16 GELU: 201 MB in 45 us).  A thread takes VE columns of every R-th row, four rows' loads of both matrices under way.
 struct SlopeArgs {
   const void* dy; const void* pre; void* dz; float* part;
   long long lddy, ldp, lddz, rows;
@@ -551,8 +551,8 @@ constexpr size_t FLAG_BYTES = (SPLIT_BLOCKS * 4 + 255) / 256 * 256;
 long long rows64(long long rows) { return (rows + 63) / 64 * 64; }
 size_t piece_bytes(long long rows, int cols) { return round256((size_t)rows64(rows) * ((cols + 7) / 8 * 8) * 6); }
 // The pieces' way is taken where its time by the models is less; plan_fma leaves out what every launch costs.  Around the border, us as plain
-// fused multiply-adds and in pieces: 256 x 512 x 512 11.0, 13.3; 1000 x 784 x 128 12.8, 15.9; 400 x 1024 x 512 24.0, 17.0; 20000 x 128 x 128
-// 32.6, 27.2; 1024 x 785 x 512 32.2, 20.2; gradients of 512 x 512 x 512 22.5, 28.2, of 1024 x 512 x 512 45.6, 34.0.
+// fused multiply-adds and in pieces: 256 x 512 x 512 10.8, 13.3; 512 x 512 x 512 13.9, 14.4; 1000 x 784 x 128 12.9, 15.9; 400 x 1024 x 512 23.4, 17.6;
+// 20000 x 128 x 128 32.4, 28.0; 1024 x 785 x 512 32.3, 20.8; gradients of 512 x 512 x 512 22.7, 28.2, of 1024 x 512 x 512 45.5, 34.4.
 constexpr double PLAIN_START = 3.0;
 double split_time(size_t bytes) { return 3.0 + (double)bytes * (10.0 / 6.0) / 4e6; }
 // matrices whose pieces and results stay well inside scratch and the copies' coordinates

@@ -9,9 +9,9 @@
 // Pieces are those of 2^16 a, so that all 24 bits of any small a, denormal ones included, are multiples of 2^-133, bf16's smallest number; the epilogue
 // takes 2^-32 of the sums.  The scaled sums overflow before those of fp32 do: infinities, NaN and elements of 2^L and more, 2 L = 94 - log2 of the terms
 // (rounded up), raise their block's flag.  The product is then taken from the fp32 matrices by fused multiply-adds instead: the results are
-// fp32's whatever the data, and the cost of such data is time (4096^3: 2.5 ms for 0.75).
+// fp32's whatever the data, and the cost of such data is time (4096^3: 3.3 ms for 0.71).
 //
-// 4096^3 with GELU: splitting 67 us (335 MB, 5 TB/s), products 565 us (1.46 PFLOP/s in bf16), epilogue 40; the plain kernel takes 2507.
+// 4096^3 with GELU: splitting 67 us (335 MB, 5 TB/s), products 590 us (1.40 PFLOP/s in bf16), epilogue 50; the plain kernel takes 2507.
 //
 // Layout: pieces [3][rows to a multiple of 64][columns to a multiple of 8], zeros behind the matrix: a block of 64 terms never reaches
 // into the next piece, whichever way the sum runs.
